@@ -338,6 +338,78 @@ DEMON_API demon_status demon_vae_crossfade(const float* d_prev_tail, long long p
                                  float* d_out, long long out_stride, int n_planes, int n_samples, void* stream);
 
 /*
+ * ---- Operators of the generator's layers in 8 bits.  In every tick of the streaming loop (section 3.1) the transformer that makes the
+ * latents runs before the decode; section 3.7 keeps its norms in fp32 and its products in fewer bits.  These are its norm, its
+ * products and the two steps that make their operands, for inference:
+ *
+ *   demon_vae_rms_norm_fp8 -> demon_vae_matmul_fp8 -> demon_vae_quantize_fp8 (gated) -> demon_vae_matmul_fp8 -> (residual of the next norm)
+ *
+ * with weights laid out once by demon_vae_quantize_weights_fp8; the last product can write the latent that demon_vae_decode reads.
+ *
+ * Format.  Values are e4m3 (1 sign, 4 exponent, 3 mantissa bits, bias 7, largest 448, NaN but no infinity), one byte each, channels
+ * fastest.  A block of 128 channels of a row (the last one may be short) has one fp32 scale, at [block][row] of its array; a 128 x 128 block
+ * of a weight matrix has one at [block of rows][block of columns].  With y in fp32:
+ *   scale = max(max over the block of |y|, 2^-100) / 448,   q = e4m3(y / scale), nearest, ties to even
+ * where y / scale is y times the rounded reciprocal of the scale.  A NaN in a block makes its scale and all its values NaN; an infinity
+ * makes the scale infinite, the infinities NaN and the other values zeros.
+ *
+ * All of them: no handle, no workspace, nothing allocated, one launch on `stream` (a stream of the current device, on which all buffers
+ * are), results that do not depend on timing.  Row strides are in elements, of any value that keeps written rows apart (an input's may be 0:
+ * one row for all); any alignment of the element type is accepted, 16-byte aligned rows are fastest.  Inputs may overlap each other, outputs
+ * nothing, unless stated.  Only rows [0, rows) and the channels named are written.  INVALID_ARG: null pointers where a buffer is needed, sizes < 1,
+ * an unknown dtype, strides that make written rows or scales overlap, a negative stride.  UNSUPPORTED: sizes beyond those stated.
+ */
+
+/*
+ * Rows in 8 bits: y = x or, with gated != 0, y = silu(gate) * up, silu(g) = g / (1 + exp(-g)), of rows [gate | up] of 2 channels values.
+ *   d_x     : device, [rows][channels] or [rows][2 channels], fp32 (DEMON_F32) or bf16 (DEMON_BF16), rows x_stride elements apart
+ *   d_q     : device, e4m3 [rows][channels], rows q_stride bytes apart
+ *   d_scale : device, fp32 [ceil(channels / 128)][rows], blocks scale_stride floats apart
+ * UNSUPPORTED: channels > 16777216.
+ */
+DEMON_API demon_status demon_vae_quantize_fp8(const void* d_x, long long x_stride, int rows, int channels, int gated, demon_dtype dtype,
+                                              void* d_q, long long q_stride, float* d_scale, long long scale_stride, void* stream);
+
+/*
+ * Root-mean-square norm with the residual's addition, its output in 8 bits:
+ *   h = x + residual,   y[c] = h[c] / sqrt(mean over the channels of h^2 + eps) * weight[c]
+ * in fp32; h is normed as it is, and rounded only for d_sum.  (A row of zeros with eps = 0 is NaN.)
+ *   d_x, d_residual : device, [rows][channels], fp32 or bf16; d_residual NULL: h = x
+ *   d_weight        : device, fp32 [channels]
+ *   d_sum           : device, h in the type of d_x, or NULL.  May be d_x or d_residual itself (same pointer and stride)
+ *   d_q, d_scale    : as for demon_vae_quantize_fp8
+ * INVALID_ARG also for eps negative, infinite or NaN.  UNSUPPORTED: channels > 32768.
+ */
+DEMON_API demon_status demon_vae_rms_norm_fp8(const void* d_x, long long x_stride, const void* d_residual, long long residual_stride,
+                                              const float* d_weight, int rows, int channels, float eps, demon_dtype dtype,
+                                              void* d_sum, long long sum_stride, void* d_q, long long q_stride,
+                                              float* d_scale, long long scale_stride, void* stream);
+
+/*
+ * A weight matrix [n][k] (fp32 or bf16, rows w_stride elements apart) in 8 bits: d_q e4m3 [n][k], rows q_stride bytes apart, and
+ * d_scale fp32 [ceil(n / 128)][ceil(k / 128)], without gaps.  UNSUPPORTED: n or k > 16777216, more than 2^31 - 1 blocks.
+ */
+DEMON_API demon_status demon_vae_quantize_weights_fp8(const void* d_w, long long w_stride, int n, int k, demon_dtype dtype,
+                                                      void* d_q, long long q_stride, float* d_scale, void* stream);
+
+/*
+ * Matrix product of 8-bit rows and weights:
+ *   out[m][j] = bias[j] + sum over blocks b of a_scale[b][m] w_scale[j / 128][b] * (sum over i in b of a[m][i] w[j][i])
+ * the inner sums on the MFMA units and the outer one in fp32, in an order that depends on the sizes, alignment and strides alone; rounded once, to nearest even.
+ *   d_a, d_a_scale : device, e4m3 [rows][k], rows a_stride bytes apart; fp32 [ceil(k / 128)][rows], blocks a_scale_stride floats apart
+ *   d_w, d_w_scale : device, e4m3 [n][k], rows w_stride bytes apart; fp32 [ceil(n / 128)][ceil(k / 128)], without gaps
+ *   d_bias         : device, fp32 [n], or NULL
+ *   d_out          : device, fp32 or bf16 (out_dtype).  n_frames = 0: [rows][n], rows out_stride elements apart.  n_frames > 0: the
+ *                    latent [rows / n_frames][n][n_frames] (the layout demon_vae_decode reads) of rows m = clip * n_frames + frame;
+ *                    out_stride is not used
+ * INVALID_ARG also if rows is no multiple of n_frames.  UNSUPPORTED: rows, n or k > 16777216.
+ */
+DEMON_API demon_status demon_vae_matmul_fp8(const void* d_a, long long a_stride, const float* d_a_scale, long long a_scale_stride,
+                                            const void* d_w, long long w_stride, const float* d_w_scale, const float* d_bias,
+                                            int rows, int n, int k, int n_frames, demon_dtype out_dtype, void* d_out, long long out_stride,
+                                            void* stream);
+
+/*
  * Test aid: after the next decode calls, copy the activation produced by layer `layer` (0-based
  * index into the sequence up_0, res_0_0 .. res_0_{n_res-1}, up_1, ...; -1 disables) of all
  * extended windows to d_dst as fp32, row-major [extended samples at that level, channels].  While it is on, calls compute the

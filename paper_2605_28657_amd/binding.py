@@ -81,6 +81,15 @@ def load_library() -> ctypes.CDLL:
                                                 ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
     lib.demon_vae_crossfade.argtypes = [ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_longlong,
                                         ctypes.c_void_p, ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_void_p]
+    LL = ctypes.c_longlong
+    lib.demon_vae_quantize_fp8.argtypes = [ctypes.c_void_p, LL, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                           ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p]
+    lib.demon_vae_rms_norm_fp8.argtypes = [ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                           ctypes.c_int, ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p]
+    lib.demon_vae_quantize_weights_fp8.argtypes = [ctypes.c_void_p, LL, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, LL,
+                                                   ctypes.c_void_p, ctypes.c_void_p]
+    lib.demon_vae_matmul_fp8.argtypes = [ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, LL, ctypes.c_void_p]
     lib.demon_vae_debug_tap.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t]
     lib.demon_vae_debug_callers_grid.argtypes = [ctypes.c_void_p, ctypes.c_int]
     lib.demon_vae_debug_last_grid.argtypes = [ctypes.c_void_p, P(ctypes.c_int), P(ctypes.c_longlong), P(ctypes.c_int)]
@@ -285,6 +294,161 @@ def crossfade(prev_tail, next_head, out=None):
     assert a.shape == b.shape == o.shape
     demon_vae_crossfade(a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), o.data_ptr(), o.stride(0),
                         a.shape[0], a.shape[1], torch.cuda.current_stream().cuda_stream)
+    return out
+
+
+def demon_vae_quantize_fp8(d_x: int, x_stride: int, rows: int, channels: int, gated: int, dtype: int, d_q: int, q_stride: int,
+                           d_scale: int, scale_stride: int, stream: int = 0):
+    _check(load_library().demon_vae_quantize_fp8(d_x, x_stride, rows, channels, gated, dtype, d_q, q_stride, d_scale, scale_stride, stream))
+
+
+def demon_vae_rms_norm_fp8(d_x: int, x_stride: int, d_residual: int, residual_stride: int, d_weight: int, rows: int, channels: int,
+                           eps: float, dtype: int, d_sum: int, sum_stride: int, d_q: int, q_stride: int, d_scale: int,
+                           scale_stride: int, stream: int = 0):
+    _check(load_library().demon_vae_rms_norm_fp8(d_x, x_stride, d_residual, residual_stride, d_weight, rows, channels, eps, dtype,
+                                                 d_sum, sum_stride, d_q, q_stride, d_scale, scale_stride, stream))
+
+
+def demon_vae_quantize_weights_fp8(d_w: int, w_stride: int, n: int, k: int, dtype: int, d_q: int, q_stride: int, d_scale: int,
+                                   stream: int = 0):
+    _check(load_library().demon_vae_quantize_weights_fp8(d_w, w_stride, n, k, dtype, d_q, q_stride, d_scale, stream))
+
+
+def demon_vae_matmul_fp8(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride: int, d_w: int, w_stride: int, d_w_scale: int,
+                         d_bias: int, rows: int, n: int, k: int, n_frames: int, out_dtype: int, d_out: int, out_stride: int,
+                         stream: int = 0):
+    _check(load_library().demon_vae_matmul_fp8(d_a, a_stride, d_a_scale, a_scale_stride, d_w, w_stride, d_w_scale, d_bias, rows, n, k,
+                                               n_frames, out_dtype, d_out, out_stride, stream))
+
+
+def _launch(fn, device, *args):
+    """fn(*args, stream) on the current stream of `device`, with that device current."""
+    import torch
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
+        fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            fn(*args, stream)
+
+
+def _matrix(t, dtypes, device=None):
+    """The row stride of a device matrix whose channels follow each other (a slice of a wider matrix is fine)."""
+    assert t.is_cuda and t.dim() == 2 and t.dtype in dtypes and (t.shape[1] == 1 or t.stride(1) == 1)
+    assert device is None or t.device == device
+    return t.stride(0)
+
+
+def _fp8_rows(rows: int, channels: int, device, out):
+    """(q, scale) to write into: given ones, checked, or new ones, rows of q 16 bytes apart or a multiple of that."""
+    import torch
+    blocks = -(-channels // 128)
+    if out is None:
+        q = torch.empty((rows, -(-channels // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :channels]
+        return q, torch.empty((blocks, rows), dtype=torch.float32, device=device)
+    q, scale = out
+    _matrix(q, (torch.float8_e4m3fn,), device)
+    assert tuple(q.shape) == (rows, channels)
+    assert tuple(scale.shape) == (blocks, rows) and scale.dtype == torch.float32 and scale.device == device and (rows == 1 or scale.stride(1) == 1)
+    return q, scale
+
+
+def _apart(stride: int, width: int, rows: int) -> int:
+    """The stride to pass for rows of `width` that are written: any, where there is but one row."""
+    return stride if rows > 1 else max(stride, width)
+
+
+def quantize_fp8(x, gated: bool = False, out=None):
+    """(q, scale): rows x [rows, channels] (fp32 or bf16), or with `gated` silu(x[:, :channels]) * x[:, channels:] of rows
+    [rows, 2 channels], as e4m3 [rows, channels] with one fp32 scale for each block of 128 channels, [blocks, rows].
+    q * scale[block] is the value.  `out`: a pair of tensors to write into."""
+    import torch
+    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[x.dtype]
+    xs = _matrix(x, (x.dtype,))
+    rows, channels = x.shape
+    if gated:
+        assert channels % 2 == 0
+        channels //= 2
+    q, scale = _fp8_rows(rows, channels, x.device, out)
+    _launch(demon_vae_quantize_fp8, x.device, x.data_ptr(), xs, rows, channels, int(gated), dtype, q.data_ptr(), _apart(q.stride(0), channels, rows),
+            scale.data_ptr(), _apart(scale.stride(0), rows, scale.shape[0]))
+    return q, scale
+
+
+def rms_norm_fp8(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=None):
+    """(q, scale, h): h = x + residual (h = None, x is normed where there is no residual), y = h / sqrt(mean(h^2) + eps) * weight as e4m3
+    with scales (see quantize_fp8).  x, residual: [rows, channels], both fp32 or both bf16; weight: fp32 [channels].  h goes to `sum_out`, which may
+    be x or residual itself, or to a new tensor; `out`: a pair (q, scale) to write into."""
+    import torch
+    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[x.dtype]
+    xs = _matrix(x, (x.dtype,))
+    rows, channels = x.shape
+    assert weight.device == x.device and weight.dtype == torch.float32 and weight.is_contiguous() and tuple(weight.shape) == (channels,)
+    rp = rs = hp = hs = 0
+    if residual is not None:
+        rs = _matrix(residual, (x.dtype,), x.device)
+        assert residual.shape == x.shape
+        rp = residual.data_ptr()
+        if sum_out is None:
+            sum_out = torch.empty((rows, channels), dtype=x.dtype, device=x.device)
+    if sum_out is not None:
+        hs = _apart(_matrix(sum_out, (x.dtype,), x.device), channels, rows)
+        assert sum_out.shape == x.shape
+        hp = sum_out.data_ptr()
+        if rows == 1:
+            xs = hs if hp == x.data_ptr() else xs
+            rs = hs if hp == rp else rs
+    q, scale = _fp8_rows(rows, channels, x.device, out)
+    _launch(demon_vae_rms_norm_fp8, x.device, x.data_ptr(), xs, rp, rs, weight.data_ptr(), rows, channels, eps, dtype, hp, hs,
+            q.data_ptr(), _apart(q.stride(0), channels, rows), scale.data_ptr(), _apart(scale.stride(0), rows, scale.shape[0]))
+    return q, scale, sum_out
+
+
+def quantize_weights_fp8(w, out=None):
+    """(q, scale): weights w [n, k] (fp32 or bf16) as e4m3 [n, k] with one fp32 scale for each 128 x 128 block, [blocks of n, blocks of k]."""
+    import torch
+    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[w.dtype]
+    ws = _matrix(w, (w.dtype,))
+    n, k = w.shape
+    shape = (-(-n // 128), -(-k // 128))
+    if out is None:
+        q = torch.empty((n, -(-k // 16) * 16), dtype=torch.float8_e4m3fn, device=w.device)[:, :k]
+        scale = torch.empty(shape, dtype=torch.float32, device=w.device)
+    else:
+        q, scale = out
+        _matrix(q, (torch.float8_e4m3fn,), w.device)
+        assert tuple(q.shape) == (n, k)
+        assert tuple(scale.shape) == shape and scale.dtype == torch.float32 and scale.device == w.device and scale.is_contiguous()
+    _launch(demon_vae_quantize_weights_fp8, w.device, w.data_ptr(), ws, n, k, dtype, q.data_ptr(), _apart(q.stride(0), k, n), scale.data_ptr())
+    return q, scale
+
+
+def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0, out=None):
+    """a w^T (+ bias) of rows (q, scale) of quantize_fp8 or rms_norm_fp8, a [rows, k], and weights (q, scale) of quantize_weights_fp8,
+    w [n, k]: [rows, n] in `dtype` (bf16, the default, or fp32), or with n_frames > 0 the latent [rows / n_frames, n, n_frames] of rows
+    clip * n_frames + frame.  bias: fp32 [n].  `out`: a tensor to write into (its dtype is taken)."""
+    import torch
+    rows, k = a.shape
+    n = w.shape[0]
+    as_, ws = _matrix(a, (torch.float8_e4m3fn,)), _matrix(w, (torch.float8_e4m3fn,), a.device)
+    assert w.shape[1] == k
+    blocks = -(-k // 128)
+    ss = _matrix(a_scale, (torch.float32,), a.device)
+    assert tuple(a_scale.shape) == (blocks, rows)
+    _matrix(w_scale, (torch.float32,), a.device)
+    assert tuple(w_scale.shape) == (-(-n // 128), blocks) and w_scale.is_contiguous()
+    assert bias is None or (bias.device == a.device and bias.dtype == torch.float32 and bias.is_contiguous() and tuple(bias.shape) == (n,))
+    assert n_frames >= 0 and (n_frames == 0 or rows % n_frames == 0)
+    shape = (rows // n_frames, n, n_frames) if n_frames else (rows, n)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=a.device)
+    assert tuple(out.shape) == shape and out.device == a.device and dtype in (None, out.dtype)
+    if n_frames:
+        assert out.is_contiguous()
+    to = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[out.dtype]
+    os_ = 0 if n_frames else _apart(_matrix(out, (out.dtype,)), n, rows)
+    _launch(demon_vae_matmul_fp8, a.device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
+            w_scale.data_ptr(), bias.data_ptr() if bias is not None else 0, rows, n, k, n_frames, to, out.data_ptr(), os_)
     return out
 
 
