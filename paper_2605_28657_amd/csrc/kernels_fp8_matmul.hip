@@ -76,6 +76,12 @@ __device__ __forceinline__ u32x4 load_piece(const uint8_t* p, int left)
     return v;
 }
 
+// 16 bytes a lane from memory to LDS, at `to` (the same in all lanes) + 16 * lane.
+__device__ __forceinline__ void request16(__amdgpu_buffer_rsrc_t rs, uint8_t* to, unsigned off, int scalar_off)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)to, 16, off, scalar_off, 0, 0);
+}
+
 __device__ __forceinline__ void store_out(uint16_t* p, float v) { *p = f32_to_bf16_bits(v); }
 __device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
 
@@ -88,12 +94,36 @@ template <typename O> __device__ __forceinline__ O* out_at(const MatmulFp8& a, l
     return out + (clip * a.n + n) * a.n_frames + frame;
 }
 
+// out[m][n .. n + 7], as far as there are columns
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8])
+{
+    typedef u32x4 loose __attribute__((aligned(2)));
+    *reinterpret_cast<loose*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8])
+{
+    typedef f32x4 loose __attribute__((aligned(4)));
+    *reinterpret_cast<loose*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<loose*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+template <typename O> __device__ __forceinline__ void store_row(const MatmulFp8& a, int m, int n, const float (&v)[8])
+{
+    O* p = out_at<O>(a, m, n);
+    if (a.n_frames == 0 && n + 8 <= a.n) store8(p, v);
+    else {
+        const long long step = a.n_frames ? a.n_frames : 1;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (n + e < a.n) store_out(p + e * step, v[e]);
+    }
+}
+
 }  // namespace
 
 // ---------------------------------------------------------------------------------- operands straight from memory
 // A workgroup of W waves takes 16 FN weight rows by 16 FM rows; each wave sums every W-th block of K, from operands that it loads into
 // registers itself, and the waves' sums are added in their order through LDS.  Reads any alignment and any K.
-template <typename O, int FN, int FM, int W>
+template <typename O, int FN, int FM, int W, int U>
 __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 {
     __shared__ f32x4 part[W][FN * FM][64];
@@ -113,26 +143,46 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
     }
     const float* pws = a.w_scale + (long long)(n0 / kBlock) * blocks;
     f32x4 acc[FN][FM] = {};
-    for (int b = wave; b < blocks; b += W) {
-        const long long at = (long long)b * kBlock;
-        const int left = (int)min((long long)a.k - at, (long long)kBlock) - piece * 16;
-        Operand<O> fw[FN], fa[FM];
+    // N blocks W apart from b on, all of their operands requested before the first MFMA; `left`: values of K from a lane's first piece on
+    auto take = [&](auto count, int b, auto load) __attribute__((always_inline)) {
+        constexpr int N = count();
+        Frag fw[N][FN], fa[N][FM];
+        float sw[N], sa[N][FM];
 #pragma unroll
-        for (int i = 0; i < FN; ++i) fw[i].set({load_piece(pw[i] + at, left), load_piece(pw[i] + at + 64, left - 64)});
+        for (int u = 0; u < N; ++u) {
+            const long long at = (long long)(b + u * W) * kBlock;
 #pragma unroll
-        for (int j = 0; j < FM; ++j) fa[j].set({load_piece(pa[j] + at, left), load_piece(pa[j] + at + 64, left - 64)});
-        const float sw = pws[b];
+            for (int i = 0; i < FN; ++i) fw[u][i] = {load(pw[i] + at, 0), load(pw[i] + at + 64, 64)};
 #pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            const float s = sw * ps[j][b * a.a_scale_stride];
+            for (int j = 0; j < FM; ++j) fa[u][j] = {load(pa[j] + at, 0), load(pa[j] + at + 64, 64)};
+            sw[u] = pws[b + u * W];
 #pragma unroll
-            for (int i = 0; i < FN; ++i) {
-                const f32x4 p = block_product(fw[i], fa[j]);
+            for (int j = 0; j < FM; ++j) sa[u][j] = ps[j][(b + u * W) * a.a_scale_stride];
+        }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(s, p[r], acc[i][j][r]);
+        for (int u = 0; u < N; ++u) {
+            Operand<O> ow[FN], oa[FM];
+#pragma unroll
+            for (int i = 0; i < FN; ++i) ow[i].set(fw[u][i]);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                oa[j].set(fa[u][j]);
+                const float s = sw[u] * sa[u][j];
+#pragma unroll
+                for (int i = 0; i < FN; ++i) {
+                    const f32x4 p = block_product(ow[i], oa[j]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(s, p[r], acc[i][j][r]);
+                }
             }
         }
-    }
+    };
+    const int whole = a.k / kBlock, left = a.k - whole * kBlock - piece * 16;
+    auto all = [](const uint8_t* p, int) __attribute__((always_inline)) { return (u32x4) * reinterpret_cast<const loose16*>(p); };
+    int b = wave;
+    for (; b + (U - 1) * W < whole; b += U * W) take(std::integral_constant<int, U>(), b, all);
+    for (; b < whole; b += W) take(std::integral_constant<int, 1>(), b, all);
+    if (b < blocks) take(std::integral_constant<int, 1>(), b, [&](const uint8_t* p, int behind) __attribute__((always_inline)) { return load_piece(p, left - behind); });
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -151,18 +201,258 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
     }
 }
 
-template <typename O> static hipError_t launch_direct(const MatmulFp8& a, hipStream_t stream)
+// ---------------------------------------------------------------------------------- operands through LDS
+// WN x WM waves of 16 FN weight rows by 16 FM rows each.  A panel is a block of K, 128 bytes, of each of the workgroup's weight rows (or rows).  LDS
+// holds three panels of weights and two of rows, and each is requested two blocks ahead: a panel of weights where the one of the block before was,
+// which the barrier at a block's start frees, a panel of rows where the current one is, which a second barrier frees once every wave has it in registers (two buffers
+// each, requested one block ahead at a block's start: 490 us for 8192 x 8192 x 8192, this 439).  The requests are spread over the MFMAs, one for every two:
+// a wave that issues them in a row stands still meanwhile, all waves at once (490 -> 460 us by itself).
+// Piece c of a row is at c ^ key of its row, with keys that are all different in 8 rows whose same piece 8 lanes read together, so that
+// they read all banks once.  MFMA rows stand for weight rows such that a lane's results of two MFMAs are 8 outputs that follow each other: rows
+// 4 g .. 4 g + 3 of MFMAs 2 t and 2 t + 1 are weight rows 32 t + 8 g .. + 7.
+// DIRECT: the pieces go from memory to LDS without registers, a wave's request is 8 rows (operands at 16-byte addresses); else through registers,
+// at any alignment.  The block that K ends in always goes through registers, with zeros behind K.
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU>
+__global__ __launch_bounds__(64 * WN * WM, EU) void matmul_tile_kernel(MatmulFp8 a)
 {
-    constexpr int FN = 2, FM = 2, W = 4;
+    constexpr int W = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM, LN = BN / 8 / W, LM = BM / 8 / W, T = FN * FM;
+    static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && kBlock % (16 * FN) == 0 && FN % 2 == 0 && W % 2 == 0, "");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[(3 * BN + 2 * BM) * kBlock];
+    auto panel_w = [&](int i) __attribute__((always_inline)) { return lds + i * (BN * kBlock); };
+    auto panel_a = [&](int i) __attribute__((always_inline)) { return lds + (3 * BN + i * BM) * kBlock; };
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, piece = lane >> 4;
+    const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM, tiles = tiles_n * tiles_m;
+    // workgroups go round the 8 XCDs: each XCD takes tiles that follow each other, which run down 8 row tiles before the next column
+    const int xcd = blockIdx.x & 7, tile = xcd * (tiles >> 3) + min(xcd, tiles & 7) + (int)(blockIdx.x >> 3);
+    const int strip = tile / (8 * tiles_n), in_strip = tile - strip * 8 * tiles_n, high = min(8, tiles_m - 8 * strip);
+    const int n0 = in_strip / high * BN, m0 = (strip * 8 + in_strip % high) * BM;
+    const int blocks = (a.k + kBlock - 1) / kBlock, whole = a.k / kBlock;
+
+    // a lane's row and piece in the wave's requests; rows behind the last: the last again, not stored
+    const uint8_t *base_w = a.w + (long long)n0 * a.w_stride, *base_a = a.a + (long long)m0 * a.a_stride;
+    auto key_w = [](int row) __attribute__((always_inline)) { return (row & 3) | (row >> 1 & 4); };
+    const int src_w = (lane & 7) ^ key_w(wave * 8 + (lane >> 3)), src_a = (lane & 7) ^ (lane >> 3);
+    const int last_w = a.n - 1 - n0, last_a = a.rows - 1 - m0;
+    unsigned off_w[LN], off_a[LM];
+#pragma unroll
+    for (int l = 0; l < LN; ++l) off_w[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_w) * a.w_stride) + src_w * 16;
+#pragma unroll
+    for (int l = 0; l < LM; ++l) off_a[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_a) * a.a_stride) + src_a * 16;
+    const __amdgpu_buffer_rsrc_t rs_w = make_rsrc(base_w, 0x7fffffff), rs_a = make_rsrc(base_a, 0x7fffffff);
+    u32x4 reg_w[LN], reg_a[LM];                              // !DIRECT: on their way to LDS
+    // past the last whole block the last one again: nothing reads it, and the loop has no branch that keeps the compiler from counting the requests
+    auto bring_w = [&](int l, int b, uint8_t* to) __attribute__((always_inline)) {
+        const int at = min(b, whole - 1) * kBlock;
+        if (DIRECT) request16(rs_w, to + (l * W + wave) * 1024, off_w[l], at);
+        else reg_w[l] = *reinterpret_cast<const loose16*>(base_w + off_w[l] + at);
+    };
+    auto bring_a = [&](int l, int b, uint8_t* to) __attribute__((always_inline)) {
+        const int at = min(b, whole - 1) * kBlock;
+        if (DIRECT) request16(rs_a, to + (l * W + wave) * 1024, off_a[l], at);
+        else reg_a[l] = *reinterpret_cast<const loose16*>(base_a + off_a[l] + at);
+    };
+    auto put = [&](uint8_t* to_w, uint8_t* to_a) __attribute__((always_inline)) {
+        if (DIRECT) return;
+#pragma unroll
+        for (int l = 0; l < LN; ++l) *reinterpret_cast<u32x4*>(to_w + (l * W + wave) * 1024 + lane * 16) = reg_w[l];
+#pragma unroll
+        for (int l = 0; l < LM; ++l) *reinterpret_cast<u32x4*>(to_a + (l * W + wave) * 1024 + lane * 16) = reg_a[l];
+    };
+
+    const int wn = wave % WN, wm = wave / WN;
+    const float* pws = a.w_scale + (long long)min((n0 + wn * 16 * FN) / kBlock, (a.n - 1) / kBlock) * blocks;
+    const float* ps[FM];
+    float s[FM], sa[FM], sw;                                 // scales of the current block; of the next one
+#pragma unroll
+    for (int j = 0; j < FM; ++j) ps[j] = a.a_scale + min(m0 + (wm * FM + j) * 16 + col, a.rows - 1);
+    auto load_scales = [&](int b) __attribute__((always_inline)) {
+        sw = pws[b];
+#pragma unroll
+        for (int j = 0; j < FM; ++j) sa[j] = ps[j][b * a.a_scale_stride];
+    };
+    auto next_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < FM; ++j) s[j] = sa[j] * sw;
+    };
+
+    f32x4 acc[FN][FM] = {}, p[4];
+    Operand<O> fa[FM], fw[2];
+    const int row_w = (col >> 2) * 8 + (col & 3), at_w = row_w * kBlock + (piece ^ key_w(row_w)) * 16, at_a = col * kBlock + (piece ^ (col & 7)) * 16;
+    auto read = [&](Operand<O>& f, const uint8_t* from, int at) __attribute__((always_inline)) {
+        f.set({*reinterpret_cast<const u32x4*>(from + at), *reinterpret_cast<const u32x4*>(from + (at ^ 64))});
+    };
+    auto read_w = [&](int i, const uint8_t* from) __attribute__((always_inline)) { read(fw[i & 1], from + (i / 2 * 32 + i % 2 * 4) * kBlock, at_w); };
+    // An MFMA's result is added three MFMAs later, when it is there without a wait.  The empty asm keeps the sum from being moved behind the barriers.
+    auto add = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[t / FM][t % FM][r] = fmaf(s[t % FM], p[t % 4][r], acc[t / FM][t % FM][r]);
+        asm volatile("" : "+v"(acc[t / FM][t % FM]));
+    };
+    // a block's MFMAs, and (AHEAD) the requests of block b + 2
+    constexpr int GAP = 2 * (LN + LM) <= T ? 2 : 1;          // a request every GAP MFMAs
+    constexpr int FREE_A = GAP * LN > FM ? GAP * LN : FM;    // every wave has its rows in registers: before this MFMA their panel is free
+    auto block = [&](const uint8_t* from_w, const uint8_t* from_a, auto ahead, int b, uint8_t* to_w, uint8_t* to_a) __attribute__((always_inline)) {
+        constexpr bool AHEAD = ahead();
+        read_w(0, from_w);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) read(fa[j], from_a + j * 16 * kBlock, at_a);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            if (t % FM == 0 && t / FM + 1 < FN) read_w(t / FM + 1, from_w);
+            if (AHEAD && t % GAP == GAP - 1 && t / GAP < LN) bring_w(t / GAP, b + 2, to_w);
+            if (AHEAD && t == FREE_A) asm volatile("s_barrier" ::: "memory");
+            if (AHEAD && t >= FREE_A && (t - FREE_A) % GAP == GAP - 1 && (t - FREE_A) / GAP < LM) bring_a((t - FREE_A) / GAP, b + 2, to_a);
+            p[t % 4] = block_product(fw[t / FM & 1], fa[t % FM]);
+            if (t >= 3) add(t - 3);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        static_assert(T >= 4 && FREE_A + GAP * LM <= T, "every request has an MFMA");
+        add(T - 3);
+        add(T - 2);
+        add(T - 1);
+    };
+
+    using std::integral_constant;
+    load_scales(0);
+    next_scales();
+    if (whole > 0) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int l = 0; l < LN; ++l) bring_w(l, b, panel_w(b));
+#pragma unroll
+            for (int l = 0; l < LM; ++l) bring_a(l, b, panel_a(b));
+            put(panel_w(b), panel_a(b));
+        }
+    }
+    int now = 0;                                             // the panel of weights of block b, b % 3
+    for (int b = 0; b < whole; ++b) {
+        // the block has landed (the next one's requests may be on their way), and nobody reads the panel of weights of the block before
+        if (DIRECT) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
+        else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        load_scales(min(b + 1, blocks - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(b & 1);
+        block(panel_w(now) + wn * 16 * FN * kBlock, to_a + wm * 16 * FM * kBlock, integral_constant<bool, true>(), b, to_w, to_a);
+        put(to_w, to_a);
+        next_scales();
+        now = now == 2 ? 0 : now + 1;
+    }
+    // the surplus requests have landed before LDS is written again or given back
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (whole < blocks) {
+#pragma unroll 1
+        for (int g = wave; g < (BN + BM) / 8; g += W) {
+            const bool of_w = g < BN / 8;
+            const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
+            const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
+            *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        block(panel_w(0) + wn * 16 * FN * kBlock, panel_a(0) + wm * 16 * FM * kBlock, integral_constant<bool, false>(), 0, lds, lds);
+    }
+
+#pragma unroll
+    for (int i = 0; i < FN; i += 2) {
+        const int n = n0 + wn * 16 * FN + i * 16 + 8 * piece;
+        float bias[8] = {};
+        if (a.bias) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) bias[e] = a.bias[min(n + e, a.n - 1)];
+        }
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int m = m0 + (wm * FM + j) * 16 + col;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4] + bias[e];
+            if (m < a.rows) store_row<O>(a, m, n, v);
+        }
+    }
+}
+
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU> static hipError_t launch_tile(const MatmulFp8& a, hipStream_t stream)
+{
+    const long long tiles = (long long)((a.n + 16 * FN * WN - 1) / (16 * FN * WN)) * ((a.rows + 16 * FM * WM - 1) / (16 * FM * WM));
+    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU>), dim3((unsigned)tiles), dim3(64 * WN * WM), 0, stream, a);
+    return hipGetLastError();
+}
+
+template <typename O, int FN, int FM, int W, int U> static hipError_t launch_direct(const MatmulFp8& a, hipStream_t stream)
+{
     const long long tiles = (long long)((a.n + 16 * FN - 1) / (16 * FN)) * ((a.rows + 16 * FM - 1) / (16 * FM));
     if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((matmul_direct_kernel<O, FN, FM, W>), dim3((unsigned)tiles), dim3(64 * W), 0, stream, a);
+    hipLaunchKernelGGL((matmul_direct_kernel<O, FN, FM, W, U>), dim3((unsigned)tiles), dim3(64 * W), 0, stream, a);
     return hipGetLastError();
+}
+
+// What a block of K of one tile takes on a GPU that is full of such tiles, in ns (8192 x 8192 x 8192 and, for fp32 and for operands at any address,
+// 4096 x 4096 x 4096).  A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU
+// decide it: 12000 x 11264 x 2048 in us by 256 x 256 284, 128 x 128 319, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 57, 46, 53, 61;
+// 300 x 11264 x 2048 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 25.5, 12.3, 9.4, 8.7.
+struct TileCost { int n, m, ns; };
+
+static int cheapest(const MatmulFp8& a, const TileCost* tiles, int count)
+{
+    int best = 0;
+    long long least = 0;
+    for (int i = 0; i < count; ++i) {
+        const long long all = (long long)((a.n + tiles[i].n - 1) / tiles[i].n) * ((a.rows + tiles[i].m - 1) / tiles[i].m);
+        const long long cost = (all + 255) / 256 * tiles[i].ns;
+        if (i == 0 || cost < least) { best = i; least = cost; }
+    }
+    return best;
+}
+
+static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipStream_t stream)
+{
+    if (!aligned) {
+        static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 640}};
+        if (cheapest(a, tiles, 2) == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
+        return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
+    }
+    static constexpr TileCost tiles[] = {{256, 256, 1750}, {128, 128, 550}, {128, 64, 340}, {64, 64, 213}};
+    switch (cheapest(a, tiles, 4)) {
+    case 0: return launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
+    case 1: return launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
+    case 2: return launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
+    default: return launch_tile<uint16_t, 2, 2, 2, 2, true, 4>(a, stream);
+    }
+}
+
+static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStream_t stream)
+{
+    if (!aligned) {
+        static constexpr TileCost tiles[] = {{128, 128, 1220}, {128, 64, 780}};
+        if (cheapest(a, tiles, 2) == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
+        return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
+    }
+    static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 64, 570}, {64, 64, 305}};
+    switch (cheapest(a, tiles, 3)) {
+    case 0: return launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
+    case 1: return launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
+    default: return launch_tile<float, 2, 2, 2, 2, true, 3>(a, stream);
+    }
+}
+
+// Few outputs go without LDS: 16 x 16 outputs a workgroup for one tile of rows (1 x 8192 x 8192 in us 14, 64 x 64 tiles 21; 8 x 11264 x 2048 7.4 and 7.9) or where
+// the GPU is not full of such workgroups (32 x 2048 x 2048 4.6 and 7.2), 32 x 16 up to 320 of them (64 x 2048 x 2048 5.4 and 7.2; 64 x 11264 x 2048, which
+// has 1408, 20 and 8.8).  So do operands whose rows lie too far apart for 32-bit offsets in a tile.
+template <typename O> static hipError_t launch(const MatmulFp8& a, hipStream_t stream)
+{
+    const bool aligned = (((uintptr_t)a.a | (uintptr_t)a.w | (uintptr_t)a.a_stride | (uintptr_t)a.w_stride) & 15) == 0;
+    const bool near = a.a_stride < (1 << 22) && a.w_stride < (1 << 22);
+    const long long rows16 = (a.rows + 15) / 16, n16 = (a.n + 15) / 16, n32 = (a.n + 31) / 32;
+    if (rows16 == 1 || rows16 * n16 <= 256) return launch_direct<O, 1, 1, 8, 2>(a, stream);
+    if (rows16 * n32 <= 320 || !near) return launch_direct<O, 2, 1, 8, 2>(a, stream);
+    return launch_tiles(a, O(), aligned, stream);
 }
 
 hipError_t launch_matmul_fp8(const MatmulFp8& a, bool bf16, hipStream_t stream)
 {
-    return bf16 ? launch_direct<uint16_t>(a, stream) : launch_direct<float>(a, stream);
+    return bf16 ? launch<uint16_t>(a, stream) : launch<float>(a, stream);
 }
 
 }  // namespace demon
