@@ -321,57 +321,76 @@ def demon_vae_matmul_fp8(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride
                                                n_frames, out_dtype, d_out, out_stride, stream))
 
 
+# These operators are called once or more in every layer on a few rows: a call's host time is part of what they are.
 def _launch(fn, device, *args):
     """fn(*args, stream) on the current stream of `device`, with that device current."""
     import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        fn(*args, stream)
+    index = device.index
+    if index == torch.cuda.current_device():
+        # the stream's address as it is, without the Stream object around it (1.7 us of a call)
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(device):
-            fn(*args, stream)
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status != DEMON_OK:
+        raise DemonError(status, demon_vae_last_error())
 
 
-def _matrix(t, dtypes, device=None):
-    """The row stride of a device matrix whose channels follow each other (a slice of a wider matrix is fine)."""
-    assert t.is_cuda and t.dim() == 2 and t.dtype in dtypes and (t.shape[1] == 1 or t.stride(1) == 1)
-    assert device is None or t.device == device
-    return t.stride(0)
+def _matrix(t, dtype, device) -> int:
+    """The row stride of a matrix on `device` whose channels follow each other (a slice of a wider matrix is fine)."""
+    stride = t.stride()
+    assert t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or t.shape[1] == 1) and t.device == device and device.type == "cuda"
+    return stride[0]
 
 
-def _fp8_rows(rows: int, channels: int, device, out):
-    """(q, scale) to write into: given ones, checked, or new ones, rows of q 16 bytes apart or a multiple of that."""
+def _demon_dtype(dtype) -> int:
+    import torch
+    if dtype is torch.bfloat16:
+        return DEMON_BF16
+    if dtype is torch.float32:
+        return DEMON_F32
+    raise KeyError(dtype)
+
+
+def _new_fp8(like, rows: int, channels: int):
+    """Rows in e4m3 to write into, 16 bytes apart or a multiple of that."""
+    import torch
+    wide = -(-channels // 16) * 16
+    q = like.new_empty((rows, wide), dtype=torch.float8_e4m3fn)
+    return q if wide == channels else q[:, :channels]
+
+
+def _fp8_rows(like, rows: int, channels: int, out):
+    """(q, its row stride, scale, its block stride) to write into: a given pair, checked, or new ones."""
     import torch
     blocks = -(-channels // 128)
     if out is None:
-        q = torch.empty((rows, -(-channels // 16) * 16), dtype=torch.float8_e4m3fn, device=device)[:, :channels]
-        return q, torch.empty((blocks, rows), dtype=torch.float32, device=device)
+        q = _new_fp8(like, rows, channels)
+        return q, q.stride(0), like.new_empty((blocks, rows), dtype=torch.float32), rows
     q, scale = out
-    _matrix(q, (torch.float8_e4m3fn,), device)
-    assert tuple(q.shape) == (rows, channels)
-    assert tuple(scale.shape) == (blocks, rows) and scale.dtype == torch.float32 and scale.device == device and (rows == 1 or scale.stride(1) == 1)
-    return q, scale
+    qs, ss = _matrix(q, torch.float8_e4m3fn, like.device), _matrix(scale, torch.float32, like.device)
+    assert q.shape == (rows, channels) and scale.shape == (blocks, rows)
+    return q, _apart(qs, channels, rows), scale, _apart(ss, rows, blocks)
 
 
 def _apart(stride: int, width: int, rows: int) -> int:
     """The stride to pass for rows of `width` that are written: any, where there is but one row."""
-    return stride if rows > 1 else max(stride, width)
+    return stride if rows > 1 or stride > width else width
 
 
 def quantize_fp8(x, gated: bool = False, out=None):
     """(q, scale): rows x [rows, channels] (fp32 or bf16), or with `gated` silu(x[:, :channels]) * x[:, channels:] of rows
     [rows, 2 channels], as e4m3 [rows, channels] with one fp32 scale for each block of 128 channels, [blocks, rows].
     q * scale[block] is the value.  `out`: a pair of tensors to write into."""
-    import torch
-    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[x.dtype]
-    xs = _matrix(x, (x.dtype,))
+    dtype = _demon_dtype(x.dtype)
+    device = x.device
+    xs = _matrix(x, x.dtype, device)
     rows, channels = x.shape
     if gated:
         assert channels % 2 == 0
         channels //= 2
-    q, scale = _fp8_rows(rows, channels, x.device, out)
-    _launch(demon_vae_quantize_fp8, x.device, x.data_ptr(), xs, rows, channels, int(gated), dtype, q.data_ptr(), _apart(q.stride(0), channels, rows),
-            scale.data_ptr(), _apart(scale.stride(0), rows, scale.shape[0]))
+    q, qs, scale, ss = _fp8_rows(x, rows, channels, out)
+    _launch(load_library().demon_vae_quantize_fp8, device, x.data_ptr(), xs, rows, channels, int(gated), dtype, q.data_ptr(), qs, scale.data_ptr(), ss)
     return q, scale
 
 
@@ -380,46 +399,46 @@ def rms_norm_fp8(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=
     with scales (see quantize_fp8).  x, residual: [rows, channels], both fp32 or both bf16; weight: fp32 [channels].  h goes to `sum_out`, which may
     be x or residual itself, or to a new tensor; `out`: a pair (q, scale) to write into."""
     import torch
-    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[x.dtype]
-    xs = _matrix(x, (x.dtype,))
-    rows, channels = x.shape
-    assert weight.device == x.device and weight.dtype == torch.float32 and weight.is_contiguous() and tuple(weight.shape) == (channels,)
-    rp = rs = hp = hs = 0
+    xt, device = x.dtype, x.device
+    dtype = _demon_dtype(xt)
+    xs = _matrix(x, xt, device)
+    rows, channels = shape = x.shape
+    assert weight.dtype is torch.float32 and weight.shape == (channels,) and weight.is_contiguous() and weight.device == device
+    xp, rp, rs, hp, hs = x.data_ptr(), 0, 0, 0, 0
     if residual is not None:
-        rs = _matrix(residual, (x.dtype,), x.device)
-        assert residual.shape == x.shape
+        rs = _matrix(residual, xt, device)
+        assert residual.shape == shape
         rp = residual.data_ptr()
         if sum_out is None:
-            sum_out = torch.empty((rows, channels), dtype=x.dtype, device=x.device)
+            sum_out = x.new_empty(shape)
     if sum_out is not None:
-        hs = _apart(_matrix(sum_out, (x.dtype,), x.device), channels, rows)
-        assert sum_out.shape == x.shape
+        hs = _apart(_matrix(sum_out, xt, device), channels, rows)
+        assert sum_out.shape == shape
         hp = sum_out.data_ptr()
-        if rows == 1:
-            xs = hs if hp == x.data_ptr() else xs
-            rs = hs if hp == rp else rs
-    q, scale = _fp8_rows(rows, channels, x.device, out)
-    _launch(demon_vae_rms_norm_fp8, x.device, x.data_ptr(), xs, rp, rs, weight.data_ptr(), rows, channels, eps, dtype, hp, hs,
-            q.data_ptr(), _apart(q.stride(0), channels, rows), scale.data_ptr(), _apart(scale.stride(0), rows, scale.shape[0]))
+        if rows == 1:                       # a single row's stride says nothing
+            xs = rs = hs
+    q, qs, scale, ss = _fp8_rows(x, rows, channels, out)
+    _launch(load_library().demon_vae_rms_norm_fp8, device, xp, xs, rp, rs, weight.data_ptr(), rows, channels, eps, dtype, hp, hs,
+            q.data_ptr(), qs, scale.data_ptr(), ss)
     return q, scale, sum_out
 
 
 def quantize_weights_fp8(w, out=None):
     """(q, scale): weights w [n, k] (fp32 or bf16) as e4m3 [n, k] with one fp32 scale for each 128 x 128 block, [blocks of n, blocks of k]."""
     import torch
-    dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[w.dtype]
-    ws = _matrix(w, (w.dtype,))
+    dtype = _demon_dtype(w.dtype)
+    device = w.device
+    ws = _matrix(w, w.dtype, device)
     n, k = w.shape
-    shape = (-(-n // 128), -(-k // 128))
+    blocks = (-(-n // 128), -(-k // 128))
     if out is None:
-        q = torch.empty((n, -(-k // 16) * 16), dtype=torch.float8_e4m3fn, device=w.device)[:, :k]
-        scale = torch.empty(shape, dtype=torch.float32, device=w.device)
+        q, scale = _new_fp8(w, n, k), w.new_empty(blocks, dtype=torch.float32)
+        qs = q.stride(0)
     else:
         q, scale = out
-        _matrix(q, (torch.float8_e4m3fn,), w.device)
-        assert tuple(q.shape) == (n, k)
-        assert tuple(scale.shape) == shape and scale.dtype == torch.float32 and scale.device == w.device and scale.is_contiguous()
-    _launch(demon_vae_quantize_weights_fp8, w.device, w.data_ptr(), ws, n, k, dtype, q.data_ptr(), _apart(q.stride(0), k, n), scale.data_ptr())
+        qs = _apart(_matrix(q, torch.float8_e4m3fn, device), k, n)
+        assert q.shape == (n, k) and scale.shape == blocks and scale.dtype is torch.float32 and scale.device == device and scale.is_contiguous()
+    _launch(load_library().demon_vae_quantize_weights_fp8, device, w.data_ptr(), ws, n, k, dtype, q.data_ptr(), qs, scale.data_ptr())
     return q, scale
 
 
@@ -428,27 +447,26 @@ def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0,
     w [n, k]: [rows, n] in `dtype` (bf16, the default, or fp32), or with n_frames > 0 the latent [rows / n_frames, n, n_frames] of rows
     clip * n_frames + frame.  bias: fp32 [n].  `out`: a tensor to write into (its dtype is taken)."""
     import torch
+    device = a.device
     rows, k = a.shape
     n = w.shape[0]
-    as_, ws = _matrix(a, (torch.float8_e4m3fn,)), _matrix(w, (torch.float8_e4m3fn,), a.device)
-    assert w.shape[1] == k
     blocks = -(-k // 128)
-    ss = _matrix(a_scale, (torch.float32,), a.device)
-    assert tuple(a_scale.shape) == (blocks, rows)
-    _matrix(w_scale, (torch.float32,), a.device)
-    assert tuple(w_scale.shape) == (-(-n // 128), blocks) and w_scale.is_contiguous()
-    assert bias is None or (bias.device == a.device and bias.dtype == torch.float32 and bias.is_contiguous() and tuple(bias.shape) == (n,))
+    as_, ws = _matrix(a, torch.float8_e4m3fn, device), _matrix(w, torch.float8_e4m3fn, device)
+    ss, _ = _matrix(a_scale, torch.float32, device), _matrix(w_scale, torch.float32, device)
+    assert w.shape[1] == k and a_scale.shape == (blocks, rows) and w_scale.shape == (-(-n // 128), blocks) and w_scale.is_contiguous()
+    assert bias is None or (bias.device == device and bias.dtype is torch.float32 and bias.is_contiguous() and bias.shape == (n,))
     assert n_frames >= 0 and (n_frames == 0 or rows % n_frames == 0)
     shape = (rows // n_frames, n, n_frames) if n_frames else (rows, n)
     if out is None:
-        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=a.device)
-    assert tuple(out.shape) == shape and out.device == a.device and dtype in (None, out.dtype)
+        out = a.new_empty(shape, dtype=dtype or torch.bfloat16)
+    assert out.shape == shape and out.device == device and dtype in (None, out.dtype)
     if n_frames:
         assert out.is_contiguous()
-    to = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[out.dtype]
-    os_ = 0 if n_frames else _apart(_matrix(out, (out.dtype,)), n, rows)
-    _launch(demon_vae_matmul_fp8, a.device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
-            w_scale.data_ptr(), bias.data_ptr() if bias is not None else 0, rows, n, k, n_frames, to, out.data_ptr(), os_)
+        os_ = 0
+    else:
+        os_ = _apart(_matrix(out, out.dtype, device), n, rows)
+    _launch(load_library().demon_vae_matmul_fp8, device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
+            w_scale.data_ptr(), 0 if bias is None else bias.data_ptr(), rows, n, k, n_frames, _demon_dtype(out.dtype), out.data_ptr(), os_)
     return out
 
 
