@@ -212,87 +212,129 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 // 4 g .. 4 g + 3 of MFMAs 2 t and 2 t + 1 are weight rows 32 t + 8 g .. + 7.
 // DIRECT: the pieces go from memory to LDS without registers, a wave's request is 8 rows (operands at 16-byte addresses); else through registers,
 // at any alignment.  The block that K ends in always goes through registers, with zeros behind K.
-template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU>
-__global__ __launch_bounds__(64 * WN * WM, EU) void matmul_tile_kernel(MatmulFp8 a)
-{
-    constexpr int W = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM, LN = BN / 8 / W, LM = BM / 8 / W, T = FN * FM;
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJob {
+    static constexpr int W = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM, LN = BN / 8 / W, LM = BM / 8 / W, T = FN * FM;
+    static constexpr int LDS_BYTES = (3 * BN + 2 * BM) * kBlock;
+    static constexpr int GAP = 3 * (LN + LM) <= T ? 3 : 2 * (LN + LM) <= T ? 2 : 1;   // a request every GAP MFMAs
+    static constexpr int FREE_A = GAP * LN > FM ? GAP * LN : FM;     // every wave has its rows in registers: before this MFMA their panel is free
     static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && kBlock % (16 * FN) == 0 && FN % 2 == 0 && W % 2 == 0, "");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[(3 * BN + 2 * BM) * kBlock];
-    auto panel_w = [&](int i) __attribute__((always_inline)) { return lds + i * (BN * kBlock); };
-    auto panel_a = [&](int i) __attribute__((always_inline)) { return lds + (3 * BN + i * BM) * kBlock; };
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, piece = lane >> 4;
-    const int tiles_n = (a.n + BN - 1) / BN, tiles_m = (a.rows + BM - 1) / BM, tiles = tiles_n * tiles_m;
-    // workgroups go round the 8 XCDs: each XCD takes tiles that follow each other, which run down 8 row tiles before the next column
-    const int xcd = blockIdx.x & 7, tile = xcd * (tiles >> 3) + min(xcd, tiles & 7) + (int)(blockIdx.x >> 3);
-    const int strip = tile / (8 * tiles_n), in_strip = tile - strip * 8 * tiles_n, high = min(8, tiles_m - 8 * strip);
-    const int n0 = in_strip / high * BN, m0 = (strip * 8 + in_strip % high) * BM;
-    const int blocks = (a.k + kBlock - 1) / kBlock, whole = a.k / kBlock;
+    static_assert(T >= 4 && FREE_A + GAP * LM <= T, "every request has an MFMA");
 
-    // a lane's row and piece in the wave's requests; rows behind the last: the last again, not stored
-    const uint8_t *base_w = a.w + (long long)n0 * a.w_stride, *base_a = a.a + (long long)m0 * a.a_stride;
-    auto key_w = [](int row) __attribute__((always_inline)) { return (row & 3) | (row >> 1 & 4); };
-    const int src_w = (lane & 7) ^ key_w(wave * 8 + (lane >> 3)), src_a = (lane & 7) ^ (lane >> 3);
-    const int last_w = a.n - 1 - n0, last_a = a.rows - 1 - m0;
+    const MatmulFp8& a;
+    uint8_t* lds;
+    const int lane, wave, col, piece, wn, wm, blocks, whole;
+    // a lane's piece in the wave's requests and its rows' offsets; of the rows behind the last one the last again, not stored
+    const int src_w, src_a, at_w, at_a;
+    int last_w, last_a;
     unsigned off_w[LN], off_a[LM];
-#pragma unroll
-    for (int l = 0; l < LN; ++l) off_w[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_w) * a.w_stride) + src_w * 16;
-#pragma unroll
-    for (int l = 0; l < LM; ++l) off_a[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_a) * a.a_stride) + src_a * 16;
-    const __amdgpu_buffer_rsrc_t rs_w = make_rsrc(base_w, 0x7fffffff), rs_a = make_rsrc(base_a, 0x7fffffff);
+    const uint8_t *base_w, *base_a;
+    __amdgpu_buffer_rsrc_t rs_w, rs_a;
     u32x4 reg_w[LN], reg_a[LM];                              // !DIRECT: on their way to LDS
-    // past the last whole block the last one again: nothing reads it, and the loop has no branch that keeps the compiler from counting the requests
-    auto bring_w = [&](int l, int b, uint8_t* to) __attribute__((always_inline)) {
-        const int at = min(b, whole - 1) * kBlock;
-        if (DIRECT) request16(rs_w, to + (l * W + wave) * 1024, off_w[l], at);
-        else reg_w[l] = *reinterpret_cast<const loose16*>(base_w + off_w[l] + at);
-    };
-    auto bring_a = [&](int l, int b, uint8_t* to) __attribute__((always_inline)) {
-        const int at = min(b, whole - 1) * kBlock;
-        if (DIRECT) request16(rs_a, to + (l * W + wave) * 1024, off_a[l], at);
-        else reg_a[l] = *reinterpret_cast<const loose16*>(base_a + off_a[l] + at);
-    };
-    auto put = [&](uint8_t* to_w, uint8_t* to_a) __attribute__((always_inline)) {
+    const float* pws;
+    unsigned ps[FM];                                         // bytes from a block's scales to a lane's row
+    float s[FM], sa[FM], sw;                                 // scales of the current block; of the next one
+    f32x4 acc[FN][FM], p[4];
+    Operand<O> fa[FM], fw[2];
+
+    static __device__ __forceinline__ int key_w(int row) { return (row & 3) | (row >> 1 & 4); }
+    static __device__ __forceinline__ int row_w(int col) { return (col >> 2) * 8 + (col & 3); }
+
+    __device__ __forceinline__ TileJob(const MatmulFp8& args, uint8_t* shared)
+        : a(args), lds(shared), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), col(lane & 15), piece(lane >> 4),
+          wn(wave % WN), wm(wave / WN), blocks((args.k + kBlock - 1) / kBlock), whole(args.k / kBlock),
+          src_w((lane & 7) ^ key_w(wave * 8 + (lane >> 3))), src_a((lane & 7) ^ (lane >> 3)),
+          at_w(row_w(col) * kBlock + (piece ^ key_w(row_w(col))) * 16), at_a(col * kBlock + (piece ^ (col & 7)) * 16) {}
+
+    __device__ __forceinline__ uint8_t* panel_w(int i) { return lds + i * (BN * kBlock); }
+    __device__ __forceinline__ uint8_t* panel_a(int i) { return lds + (3 * BN + i * BM) * kBlock; }
+
+    // requests and scales from here on are those of the tile at weight row n0 and row m0
+    __device__ __forceinline__ void aim_requests(int n0, int m0)
+    {
+        base_w = a.w + (long long)n0 * a.w_stride;
+        base_a = a.a + (long long)m0 * a.a_stride;
+        rs_w = make_rsrc(base_w, 0x7fffffff);
+        rs_a = make_rsrc(base_a, 0x7fffffff);
+        last_w = a.n - 1 - n0;
+        last_a = a.rows - 1 - m0;
+#pragma unroll
+        for (int l = 0; l < LN; ++l) off_w[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_w) * a.w_stride) + src_w * 16;
+#pragma unroll
+        for (int l = 0; l < LM; ++l) off_a[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_a) * a.a_stride) + src_a * 16;
+    }
+    __device__ __forceinline__ void aim_scales(int n0, int m0)
+    {
+        pws = a.w_scale + (long long)min((n0 + wn * 16 * FN) / kBlock, (a.n - 1) / kBlock) * blocks;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) ps[j] = (unsigned)min(m0 + (wm * FM + j) * 16 + col, a.rows - 1) * 4;
+    }
+
+    __device__ __forceinline__ void bring_w(int l, int b, uint8_t* to)
+    {
+        if (DIRECT) request16(rs_w, to + (l * W + wave) * 1024, off_w[l], b * kBlock);
+        else reg_w[l] = *reinterpret_cast<const loose16*>(base_w + off_w[l] + b * kBlock);
+    }
+    __device__ __forceinline__ void bring_a(int l, int b, uint8_t* to)
+    {
+        if (DIRECT) request16(rs_a, to + (l * W + wave) * 1024, off_a[l], b * kBlock);
+        else reg_a[l] = *reinterpret_cast<const loose16*>(base_a + off_a[l] + b * kBlock);
+    }
+    __device__ __forceinline__ void put(uint8_t* to_w, uint8_t* to_a)
+    {
         if (DIRECT) return;
 #pragma unroll
         for (int l = 0; l < LN; ++l) *reinterpret_cast<u32x4*>(to_w + (l * W + wave) * 1024 + lane * 16) = reg_w[l];
 #pragma unroll
         for (int l = 0; l < LM; ++l) *reinterpret_cast<u32x4*>(to_a + (l * W + wave) * 1024 + lane * 16) = reg_a[l];
-    };
-
-    const int wn = wave % WN, wm = wave / WN;
-    const float* pws = a.w_scale + (long long)min((n0 + wn * 16 * FN) / kBlock, (a.n - 1) / kBlock) * blocks;
-    const float* ps[FM];
-    float s[FM], sa[FM], sw;                                 // scales of the current block; of the next one
-#pragma unroll
-    for (int j = 0; j < FM; ++j) ps[j] = a.a_scale + min(m0 + (wm * FM + j) * 16 + col, a.rows - 1);
-    auto load_scales = [&](int b) __attribute__((always_inline)) {
+    }
+    __device__ __forceinline__ void load_scales(int b)
+    {
         sw = pws[b];
+        const char* of_block = (const char*)(a.a_scale + b * a.a_scale_stride);
 #pragma unroll
-        for (int j = 0; j < FM; ++j) sa[j] = ps[j][b * a.a_scale_stride];
-    };
-    auto next_scales = [&]() __attribute__((always_inline)) {
+        for (int j = 0; j < FM; ++j) sa[j] = *reinterpret_cast<const float*>(of_block + ps[j]);
+    }
+    __device__ __forceinline__ void next_scales()
+    {
 #pragma unroll
         for (int j = 0; j < FM; ++j) s[j] = sa[j] * sw;
-    };
+    }
 
-    f32x4 acc[FN][FM] = {}, p[4];
-    Operand<O> fa[FM], fw[2];
-    const int row_w = (col >> 2) * 8 + (col & 3), at_w = row_w * kBlock + (piece ^ key_w(row_w)) * 16, at_a = col * kBlock + (piece ^ (col & 7)) * 16;
-    auto read = [&](Operand<O>& f, const uint8_t* from, int at) __attribute__((always_inline)) {
+    // requests the first two blocks; nobody reads LDS
+    __device__ __forceinline__ void prime()
+    {
+        load_scales(0);
+        if (whole > 0) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int l = 0; l < LN; ++l) bring_w(l, min(b, whole - 1), panel_w(b));
+#pragma unroll
+                for (int l = 0; l < LM; ++l) bring_a(l, min(b, whole - 1), panel_a(b));
+                put(panel_w(b), panel_a(b));
+            }
+        }
+    }
+
+    __device__ __forceinline__ void read(Operand<O>& f, const uint8_t* from, int at)
+    {
         f.set({*reinterpret_cast<const u32x4*>(from + at), *reinterpret_cast<const u32x4*>(from + (at ^ 64))});
-    };
-    auto read_w = [&](int i, const uint8_t* from) __attribute__((always_inline)) { read(fw[i & 1], from + (i / 2 * 32 + i % 2 * 4) * kBlock, at_w); };
+    }
+    __device__ __forceinline__ void read_w(int i, const uint8_t* from) { read(fw[i & 1], from + (i / 2 * 32 + i % 2 * 4) * kBlock, at_w); }
+
     // An MFMA's result is added three MFMAs later, when it is there without a wait.  The empty asm keeps the sum from being moved behind the barriers.
-    auto add = [&](int t) __attribute__((always_inline)) {
+    __device__ __forceinline__ void add(int t)
+    {
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[t / FM][t % FM][r] = fmaf(s[t % FM], p[t % 4][r], acc[t / FM][t % FM][r]);
         asm volatile("" : "+v"(acc[t / FM][t % FM]));
-    };
-    // a block's MFMAs, and (AHEAD) the requests of block b + 2
-    constexpr int GAP = 2 * (LN + LM) <= T ? 2 : 1;          // a request every GAP MFMAs
-    constexpr int FREE_A = GAP * LN > FM ? GAP * LN : FM;    // every wave has its rows in registers: before this MFMA their panel is free
-    auto block = [&](const uint8_t* from_w, const uint8_t* from_a, auto ahead, int b, uint8_t* to_w, uint8_t* to_a) __attribute__((always_inline)) {
-        constexpr bool AHEAD = ahead();
+    }
+
+    // a block's MFMAs, and (AHEAD) the requests of block `next`
+    template <bool AHEAD> __device__ __forceinline__ void block(const uint8_t* from_w, const uint8_t* from_a, int next, uint8_t* to_w, uint8_t* to_a)
+    {
+        from_w += wn * 16 * FN * kBlock;
+        from_a += wm * 16 * FM * kBlock;
         read_w(0, from_w);
 #pragma unroll
         for (int j = 0; j < FM; ++j) read(fa[j], from_a + j * 16 * kBlock, at_a);
@@ -300,75 +342,176 @@ __global__ __launch_bounds__(64 * WN * WM, EU) void matmul_tile_kernel(MatmulFp8
 #pragma unroll
         for (int t = 0; t < T; ++t) {
             if (t % FM == 0 && t / FM + 1 < FN) read_w(t / FM + 1, from_w);
-            if (AHEAD && t % GAP == GAP - 1 && t / GAP < LN) bring_w(t / GAP, b + 2, to_w);
+            if (AHEAD && t % GAP == GAP - 1 && t / GAP < LN) bring_w(t / GAP, next, to_w);
             if (AHEAD && t == FREE_A) asm volatile("s_barrier" ::: "memory");
-            if (AHEAD && t >= FREE_A && (t - FREE_A) % GAP == GAP - 1 && (t - FREE_A) / GAP < LM) bring_a((t - FREE_A) / GAP, b + 2, to_a);
+            if (AHEAD && t >= FREE_A && (t - FREE_A) % GAP == GAP - 1 && (t - FREE_A) / GAP < LM) bring_a((t - FREE_A) / GAP, next, to_a);
             p[t % 4] = block_product(fw[t / FM & 1], fa[t % FM]);
             if (t >= 3) add(t - 3);
             __builtin_amdgcn_sched_barrier(0);
         }
-        static_assert(T >= 4 && FREE_A + GAP * LM <= T, "every request has an MFMA");
         add(T - 3);
         add(T - 2);
         add(T - 1);
-    };
-
-    using std::integral_constant;
-    load_scales(0);
-    next_scales();
-    if (whole > 0) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-#pragma unroll
-            for (int l = 0; l < LN; ++l) bring_w(l, b, panel_w(b));
-#pragma unroll
-            for (int l = 0; l < LM; ++l) bring_a(l, b, panel_a(b));
-            put(panel_w(b), panel_a(b));
-        }
     }
-    int now = 0;                                             // the panel of weights of block b, b % 3
-    for (int b = 0; b < whole; ++b) {
-        // the block has landed (the next one's requests may be on their way), and nobody reads the panel of weights of the block before
-        if (DIRECT) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
-        else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        load_scales(min(b + 1, blocks - 1));
-        __builtin_amdgcn_sched_barrier(0);
-        uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(b & 1);
-        block(panel_w(now) + wn * 16 * FN * kBlock, to_a + wm * 16 * FM * kBlock, integral_constant<bool, true>(), b, to_w, to_a);
-        put(to_w, to_a);
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // the tile's sums, from the blocks that prime() requested on; nobody reads LDS behind it
+    __device__ __forceinline__ void multiply()
+    {
+        clear();
         next_scales();
-        now = now == 2 ? 0 : now + 1;
-    }
-    // the surplus requests have landed before LDS is written again or given back
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (whole < blocks) {
-#pragma unroll 1
-        for (int g = wave; g < (BN + BM) / 8; g += W) {
-            const bool of_w = g < BN / 8;
-            const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
-            const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
-            *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
+        int now = 0;                                         // the panel of weights of block b, b % 3
+        for (int b = 0; b < whole; ++b) {
+            // the block has landed (the next one's requests may be on their way), and nobody reads the panel of weights of the block before
+            if (DIRECT) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
+            else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            load_scales(min(b + 1, blocks - 1));
+            __builtin_amdgcn_sched_barrier(0);
+            uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(b & 1);
+            // past the last whole block the last one again, which nothing reads: with a branch the compiler could not count the requests
+            block<true>(panel_w(now), to_a, min(b + 2, whole - 1), to_w, to_a);
+            put(to_w, to_a);
+            next_scales();
+            now = now == 2 ? 0 : now + 1;
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        block(panel_w(0) + wn * 16 * FN * kBlock, panel_a(0) + wm * 16 * FM * kBlock, integral_constant<bool, false>(), 0, lds, lds);
+        // the surplus requests have landed before LDS is written again or given back
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (whole < blocks) {
+#pragma unroll 1
+            for (int g = wave; g < (BN + BM) / 8; g += W) {
+                const bool of_w = g < BN / 8;
+                const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
+                const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
+                *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            block<false>(panel_w(0), panel_a(0), 0, lds, lds);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
     }
 
-#pragma unroll
-    for (int i = 0; i < FN; i += 2) {
-        const int n = n0 + wn * 16 * FN + i * 16 + 8 * piece;
-        float bias[8] = {};
-        if (a.bias) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) bias[e] = a.bias[min(n + e, a.n - 1)];
+    // The same where K is two whole blocks or more and another tile, at (n1, m1), follows: its first two blocks are requested in this one's last two.
+    // now, odd: the panels of this tile's first block, then of the next one's.  stores: those issued since the last request, at least.
+    __device__ __forceinline__ void multiply_on(int& now, int& odd, bool stores, int n1, int m1)
+    {
+        clear();
+        for (int b = 0; b < whole; ++b) {
+            if (b == whole - 2) aim_requests(n1, m1);
+            if (b == whole - 1) aim_scales(n1, m1);
+            if (b == 0 && stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM + FN / 2 * FM) : "memory");
+            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
+            load_scales(b + 1 < whole ? b + 1 : 0);
+            __builtin_amdgcn_sched_barrier(0);
+            uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(odd);
+            block<true>(panel_w(now), to_a, b + 2 < whole ? b + 2 : b + 2 - whole, to_w, to_a);
+            next_scales();
+            now = now == 2 ? 0 : now + 1;
+            odd ^= 1;
         }
+    }
+
+    // Whether the tile's rows lie in the output from end to end: then store() issues FN / 2 * FM stores (fp32: twice as many) and no load but the bias'.
+    __device__ __forceinline__ bool inside(int n0, int m0) { return a.n_frames == 0 && n0 + BN <= a.n && m0 + BM <= a.rows; }
+
+    __device__ __forceinline__ void store(int n0, int m0, const float* bias_of_n)
+    {
+        const bool in = inside(n0, m0);
 #pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            const int m = m0 + (wm * FM + j) * 16 + col;
-            float v[8];
+        for (int i = 0; i < FN; i += 2) {
+            const int n = n0 + wn * 16 * FN + i * 16 + 8 * piece;
+            float bias[8] = {};
+            if (bias_of_n) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4] + bias[e];
-            if (m < a.rows) store_row<O>(a, m, n, v);
+                for (int e = 0; e < 8; ++e) bias[e] = bias_of_n[min(n + e, a.n - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < FM; ++j) {
+                const int m = m0 + (wm * FM + j) * 16 + col;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4] + bias[e];
+                if (in) store8((O*)a.out + m * a.out_stride + n, v);
+                else if (m < a.rows) store_row<O>(a, m, n, v);
+            }
         }
+    }
+};
+
+// Tile `tile` of a grid of tiles_n x tiles_m: down 8 row tiles before the next column, so that the tiles that an XCD has at a time share rows and weights in its L2.
+__device__ __forceinline__ void place(int tile, int tiles_n, int tiles_m, int& at_n, int& at_m)
+{
+    const int strip = tile / (8 * tiles_n), in_strip = tile - strip * 8 * tiles_n, high = min(8, tiles_m - 8 * strip);
+    at_n = in_strip / high;
+    at_m = strip * 8 + in_strip % high;
+}
+
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU>
+__global__ __launch_bounds__(64 * WN * WM, EU) void matmul_tile_kernel(MatmulFp8 a)
+{
+    typedef TileJob<O, WN, WM, FN, FM, DIRECT> Job;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[Job::LDS_BYTES];
+    // workgroups go round the 8 XCDs: each XCD takes tiles that follow each other
+    const int tiles_n = (a.n + Job::BN - 1) / Job::BN, tiles_m = (a.rows + Job::BM - 1) / Job::BM, tiles = tiles_n * tiles_m, xcd = blockIdx.x & 7;
+    int n, m;
+    place(xcd * (tiles >> 3) + min(xcd, tiles & 7) + (int)(blockIdx.x >> 3), tiles_n, tiles_m, n, m);
+    Job job(a, lds);
+    job.aim_requests(n * Job::BN, m * Job::BM);
+    job.aim_scales(n * Job::BN, m * Job::BM);
+    job.prime();
+    job.multiply();
+    job.store(n * Job::BN, m * Job::BM, a.bias);
+}
+
+// The 256 x 256 tiles, of which a CU holds one, where K is two whole blocks or more: a workgroup for each CU that takes tile after tile of its XCD's, with no break in
+// its requests.  Up to 8 tiles that an XCD has left over behind its last whole round of 32 are cut in four for all of its CUs.  (12000 x 11264 x 2048, 8.08 rounds: a
+// workgroup a tile 287 us, this 258; 1500 x 11264 x 2048, 1.03 rounds: 58 and 43.)
+// BIAS: without it a tile's end has nothing that would wait for the requests of the next one.
+template <bool BIAS> __global__ __launch_bounds__(512, 2) void matmul_rounds_kernel(MatmulFp8 a)
+{
+    typedef TileJob<uint16_t, 2, 4, 8, 4, true> Job;
+    typedef TileJob<uint16_t, 2, 4, 4, 2, true> Part;
+    static_assert(Job::BN == 2 * Part::BN && Job::BM == 2 * Part::BM && Part::LDS_BYTES <= Job::LDS_BYTES, "");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[Job::LDS_BYTES];
+    const int tiles_n = (a.n + Job::BN - 1) / Job::BN, tiles_m = (a.rows + Job::BM - 1) / Job::BM, tiles = tiles_n * tiles_m;
+    const int xcd = blockIdx.x & 7, cu = blockIdx.x >> 3, first = xcd * (tiles >> 3) + min(xcd, tiles & 7), mine = (tiles >> 3) + (xcd < (tiles & 7) ? 1 : 0);
+    const int left = (mine & 31) <= 8 ? mine & 31 : 0, whole = mine - left;
+    if (cu < whole) {
+        Job job(a, lds);
+        int n, m, now = 0, odd = 0;
+        place(first + cu, tiles_n, tiles_m, n, m);
+        job.aim_requests(n * Job::BN, m * Job::BM);
+        job.aim_scales(n * Job::BN, m * Job::BM);
+        job.prime();
+        job.next_scales();
+        bool stores = false;
+        for (int t = cu; t < whole; t += 32) {
+            const int n0 = n * Job::BN, m0 = m * Job::BM;
+            place(first + min(t + 32, whole - 1), tiles_n, tiles_m, n, m);      // behind the last tile requests that nothing reads
+            job.multiply_on(now, odd, stores, n * Job::BN, m * Job::BM);
+            job.store(n0, m0, BIAS ? a.bias : nullptr);
+            stores = job.inside(n0, m0);
+            if (!stores) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (cu < 4 * left) {
+        int n, m;
+        place(first + whole + cu / 4, tiles_n, tiles_m, n, m);
+        const int n0 = n * Job::BN + (cu & 1) * Part::BN, m0 = m * Job::BM + (cu >> 1 & 1) * Part::BM;
+        if (n0 >= a.n || m0 >= a.rows) return;
+        Part job(a, lds);
+        job.aim_requests(n0, m0);
+        job.aim_scales(n0, m0);
+        job.prime();
+        job.multiply();
+        job.store(n0, m0, BIAS ? a.bias : nullptr);
     }
 }
 
@@ -377,6 +520,14 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU> stati
     const long long tiles = (long long)((a.n + 16 * FN * WN - 1) / (16 * FN * WN)) * ((a.rows + 16 * FM * WM - 1) / (16 * FM * WM));
     if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
     hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU>), dim3((unsigned)tiles), dim3(64 * WN * WM), 0, stream, a);
+    return hipGetLastError();
+}
+
+static hipError_t launch_rounds(const MatmulFp8& a, hipStream_t stream)
+{
+    const long long tiles = (long long)((a.n + 255) / 256) * ((a.rows + 255) / 256);
+    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(a.bias ? matmul_rounds_kernel<true> : matmul_rounds_kernel<false>, dim3(256), dim3(512), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -390,17 +541,19 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 
 // What a block of K of one tile takes on a GPU that is full of such tiles, in ns (8192 x 8192 x 8192 and, for fp32 and for operands at any address,
 // 4096 x 4096 x 4096).  A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU
-// decide it: 12000 x 11264 x 2048 in us by 256 x 256 284, 128 x 128 319, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 57, 46, 53, 61;
-// 300 x 11264 x 2048 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 25.5, 12.3, 9.4, 8.7.
+// decide it: 12000 x 11264 x 2048 in us by 256 x 256 in rounds 258, a workgroup a tile 287, 128 x 128 318, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 43, 58, 47, 53, 61;
+// 1500 x 2048 x 5632 -, 59, 26.7, 28.5, 30; 300 x 11264 x 2048 -, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 -, 25.5, 12.3, 9.4, 8.7.
 struct TileCost { int n, m, ns; };
 
-static int cheapest(const MatmulFp8& a, const TileCost* tiles, int count)
+static int cheapest(const MatmulFp8& a, const TileCost* tiles, int count, bool first_in_rounds)
 {
     int best = 0;
     long long least = 0;
     for (int i = 0; i < count; ++i) {
         const long long all = (long long)((a.n + tiles[i].n - 1) / tiles[i].n) * ((a.rows + tiles[i].m - 1) / tiles[i].m);
-        const long long cost = (all + 255) / 256 * tiles[i].ns;
+        long long cost = (all + 255) / 256 * tiles[i].ns;
+        // matmul_rounds_kernel: a last round of up to 8 tiles an XCD takes two fifths of a round
+        if (const long long left = (all + 7) / 8 % 32; i == 0 && first_in_rounds && left > 0 && left <= 8) cost -= tiles[i].ns * 3 / 5;
         if (i == 0 || cost < least) { best = i; least = cost; }
     }
     return best;
@@ -410,12 +563,13 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 640}};
-        if (cheapest(a, tiles, 2) == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false) == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
     }
     static constexpr TileCost tiles[] = {{256, 256, 1750}, {128, 128, 550}, {128, 64, 340}, {64, 64, 213}};
-    switch (cheapest(a, tiles, 4)) {
-    case 0: return launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
+    const bool rounds = a.k % kBlock == 0 && a.k >= 2 * kBlock;
+    switch (cheapest(a, tiles, 4, rounds)) {
+    case 0: return rounds ? launch_rounds(a, stream) : launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
     case 1: return launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
     case 2: return launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
     default: return launch_tile<uint16_t, 2, 2, 2, 2, true, 4>(a, stream);
@@ -426,11 +580,11 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 1220}, {128, 64, 780}};
-        if (cheapest(a, tiles, 2) == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false) == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
     }
     static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 64, 570}, {64, 64, 305}};
-    switch (cheapest(a, tiles, 3)) {
+    switch (cheapest(a, tiles, 3, false)) {
     case 0: return launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
     case 1: return launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
     default: return launch_tile<float, 2, 2, 2, 2, true, 3>(a, stream);

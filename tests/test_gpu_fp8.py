@@ -425,3 +425,23 @@ def test_wrong_tensors_are_refused():
         assert e.value.status == pa.DEMON_ERR_INVALID_ARG
     with pytest.raises(pa.DemonError):                               # written rows that overlap
         pa.matmul_fp8(a, sa, w, sw, out=torch.zeros(64, device=DEV).as_strided((4, 8), (4, 1)))
+
+
+# tiles in rounds (K a multiple of 128 from 256 on, many tiles): a last round cut in parts or not, ragged edges, K of 2, 3 and more blocks
+@pytest.mark.parametrize("rows,n,k", [(4096, 4096, 256), (4100, 4090, 384), (4097, 4352, 256), (5000, 6200, 512), (2050, 8200, 640), (8200, 8200, 256)])
+def test_product_in_rounds(rows, n, k):
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    for again in range(2):
+        a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+        bias = torch.randint(-9, 10, (n,), generator=g).float().to(DEV)
+        # whole numbers of quarters below 2^24: fp32 has them exactly, and so has a product of fp32 matrices
+        want = (a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()
+        assert float(want.abs().max()) < 2 ** 14
+        for b in (None, bias):
+            got = pa.matmul_fp8(a, sa, w, sw, bias=b)
+            assert torch.equal(got, (want if b is None else want + b).bfloat16())
+    if rows % 5 == 0:
+        latent = pa.matmul_fp8(a, sa, w, sw, n_frames=rows // 5)
+        assert torch.equal(latent, want.bfloat16().view(5, rows // 5, n).transpose(1, 2))
