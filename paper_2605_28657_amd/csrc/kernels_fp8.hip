@@ -23,18 +23,32 @@ constexpr int kBlock = 128;
 constexpr float kLargest = 448.f;
 constexpr uint32_t kFloorBits = (127 - 100) << 23;          // 2^-100
 
+// Rows of more than this are read past the caches: what comes last would push out what came first before anything finds it there, and their lines would
+// take the place of the results (gate of 12000 x 5632 rows, 270 MB: 63.4 -> 55.3 us, norm of 12000 x 2048 with a residual, 98 MB: 35.2 -> 31.2; rows of
+// 12000 x 2048, 49 MB, which the 256 MB of the last cache may well hold from whoever wrote them, 12.7 -> 14.2).
+constexpr long long kStreamBytes = 64ll << 20;
+
 template <typename T> struct Chunk;                          // 8 channels as they lie in memory
 template <> struct Chunk<uint16_t> {
     typedef u32x4 loose __attribute__((aligned(2)));
     u32x4 v = {};
-    __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const loose*>(p); }
+    template <bool STREAM = false> __device__ void load(const uint16_t* p)
+    {
+        const loose* q = reinterpret_cast<const loose*>(p);
+        v = STREAM ? (u32x4)__builtin_nontemporal_load(q) : (u32x4)*q;
+    }
     __device__ float get(int e) const { return __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16); }
     __device__ void set(int e, uint16_t x) { v[e / 2] = e & 1 ? (v[e / 2] & 0xffffu) | (uint32_t)x << 16 : (v[e / 2] & 0xffff0000u) | x; }
 };
 template <> struct Chunk<float> {
     typedef u32x4 loose __attribute__((aligned(4)));
     u32x4 v[2] = {};
-    __device__ void load(const float* p) { v[0] = *reinterpret_cast<const loose*>(p); v[1] = *reinterpret_cast<const loose*>(p + 4); }
+    template <bool STREAM = false> __device__ void load(const float* p)
+    {
+        const loose *q = reinterpret_cast<const loose*>(p), *r = reinterpret_cast<const loose*>(p + 4);
+        v[0] = STREAM ? (u32x4)__builtin_nontemporal_load(q) : (u32x4)*q;
+        v[1] = STREAM ? (u32x4)__builtin_nontemporal_load(r) : (u32x4)*r;
+    }
     __device__ float get(int e) const { return __uint_as_float(v[e / 4][e % 4]); }
     __device__ void set(int e, float x) { v[e / 4][e % 4] = __float_as_uint(x); }
 };
@@ -83,7 +97,19 @@ __device__ __forceinline__ uint32_t magnitude(const float (&y)[8])
     return m;
 }
 
-__device__ __forceinline__ float scale_of(uint32_t largest) { return __uint_as_float(umax(largest, kFloorBits)) / kLargest; }
+// One multiplication by the rounded 1 / 448: off by less than 2 steps of 2^-24 from the quotient, which costs ten instructions.
+__device__ __forceinline__ float scale_of(uint32_t largest) { return __uint_as_float(umax(largest, kFloorBits)) * (1.f / kLargest); }
+
+// 1 / scale within a step: the hardware's reciprocal, which is off by up to two, and one Newton step.  0 for an infinite scale.
+__device__ __forceinline__ float inverse(float scale)
+{
+    const float r = __builtin_amdgcn_rcpf(scale);
+    return r == 0.f ? 0.f : fmaf(fmaf(-scale, r, 1.f), r, r);
+}
+
+// g / (1 + exp(-g)), the exponential and the reciprocal as the hardware has them: off by a few steps of 2^-24 (and of the exponent's rounding, 2^-24 |g| log2 e),
+// the value's 8 bits keep 2^-4
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f)); }
 
 // Writes the first n (at most 8) values of a chunk.
 __device__ __forceinline__ void store_q(uint8_t* p, const float (&y)[8], float inv, int n)
@@ -108,8 +134,9 @@ __device__ __forceinline__ void store_q(uint8_t* p, const float (&y)[8], float i
 
 // ---------------------------------------------------------------------------------- rows, with or without a gate
 // y = x, or y = g / (1 + exp(-g)) * u of rows [g | u].  Blocks have nothing to do with each other: a workgroup's 16 groups of lanes take
-// 2^log2_rows rows, side by side in the scales [blocks, rows] that they write, by 16 / 2^log2_rows blocks, U times.
-template <typename T, bool GATED, int U>
+// 2^log2_rows rows by 16 / 2^log2_rows blocks, U times, all requested before the first is used; as few rows as their blocks fill it, since long runs of a row
+// count for more than scales of rows side by side (gate of 12000 x 5632 rows: 16 rows 70.5 us, 4 69.7, 1 63.4: 5360 GB/s, a copy of its size 5390).
+template <typename T, bool GATED, bool STREAM, int U>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ x, long long x_stride, int rows, int channels, uint8_t* __restrict__ q,
                                                             long long q_stride, float* __restrict__ scale, long long scale_stride, int log2_rows)
 {
@@ -123,8 +150,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
     for (int u = 0; u < U; ++u) {
         const long long c = (long long)(first + u * step) * kBlock + lane * 8;
         if (c + 8 <= channels) {
-            a[u].load(p + c);
-            if (GATED) b[u].load(p + channels + c);
+            a[u].template load<STREAM>(p + c);
+            if (GATED) b[u].template load<STREAM>(p + channels + c);
         } else if (c < channels) {
             load_tail(a[u], p + c, (int)(channels - c));
             if (GATED) load_tail(b[u], p + channels + c, (int)(channels - c));
@@ -138,34 +165,41 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             y[e] = a[u].get(e);
-            if (GATED) y[e] = y[e] / (1.f + __expf(-y[e])) * b[u].get(e);
+            if (GATED) y[e] = silu(y[e]) * b[u].get(e);
         }
         const float s = scale_of(max16(magnitude(y)));
         if (lane == 0) scale[block * scale_stride + row] = s;
-        store_q(q + row * q_stride + c, y, 1.f / s, (int)(channels - c));
+        store_q(q + row * q_stride + c, y, inverse(s), (int)(channels - c));
     }
 }
 
 hipError_t launch_quantize_fp8(const RowsFp8& a, const void* x, long long x_stride, bool gated, bool bf16, hipStream_t stream)
 {
     constexpr int U = 4;
+    const int blocks = (a.channels + kBlock - 1) / kBlock;
     int log2_rows = 0;
-    while (log2_rows < 4 && (1 << log2_rows) < a.rows) ++log2_rows;
-    const int blocks = (a.channels + kBlock - 1) / kBlock, span = (16 >> log2_rows) * U;
+    while (log2_rows < 4 && (16 >> (log2_rows + 1)) * U >= blocks && (1 << log2_rows) < a.rows) ++log2_rows;
+    const int span = (16 >> log2_rows) * U;
     const dim3 grid((unsigned)((a.rows + (1ll << log2_rows) - 1) >> log2_rows), (unsigned)((blocks + span - 1) / span));
+    const bool stream_in = (long long)a.rows * a.channels * (gated ? 2 : 1) * (bf16 ? 2 : 4) > kStreamBytes;
     auto go = [&](auto kernel, auto* p) {
         hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p, x_stride, a.rows, a.channels, a.q, a.q_stride, a.scale, a.scale_stride, log2_rows);
     };
-    if (bf16) gated ? go(quantize_rows_kernel<uint16_t, true, U>, (const uint16_t*)x) : go(quantize_rows_kernel<uint16_t, false, U>, (const uint16_t*)x);
-    else gated ? go(quantize_rows_kernel<float, true, U>, (const float*)x) : go(quantize_rows_kernel<float, false, U>, (const float*)x);
+    auto by_size = [&](auto* p) {
+        typedef std::remove_const_t<std::remove_pointer_t<decltype(p)>> T;
+        if (gated) stream_in ? go(quantize_rows_kernel<T, true, true, U>, p) : go(quantize_rows_kernel<T, true, false, U>, p);
+        else stream_in ? go(quantize_rows_kernel<T, false, true, U>, p) : go(quantize_rows_kernel<T, false, false, U>, p);
+    };
+    bf16 ? by_size((const uint16_t*)x) : by_size((const float*)x);
     return hipGetLastError();
 }
 
 // ---------------------------------------------------------------------------------- root-mean-square norm
 // h = x + residual;  y = h / sqrt(mean(h^2) + eps) * weight, in 8 bits.  A row belongs to N threads that hold it in registers (V chunks
 // each) from its one read to its one write; h is summed, squared and normed as it is before it is rounded for `sum`.  A thread writes
-// of `sum` what it has read of x and residual, so that `sum` may be either of them.
-template <typename T, int N, int V>
+// of `sum` what it has read of x and residual, so that `sum` may be either of them.  12000 x 2048 bf16 rows with a residual, 173 MB: 31.2 us, 5550 GB/s with two
+// waves a row, 32.2 with one, 32.8 with four.
+template <typename T, int N, int V, bool STREAM>
 __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x, long long x_stride, const T* residual, long long residual_stride,
                                                                      const float* __restrict__ weight, int rows, int channels, float eps,
                                                                      T* sum, long long sum_stride, uint8_t* __restrict__ q, long long q_stride,
@@ -173,8 +207,8 @@ __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x,
 {
     constexpr int R = N < 256 ? 256 / N : 1;
     const int t = threadIdx.x % N;
-    const long long row = (long long)blockIdx.x * R + threadIdx.x / N;
-    if (N <= 64 && row >= rows) return;                     // a row to a wave; larger groups are the whole workgroup, which has a row
+    const long long mine = (long long)blockIdx.x * R + threadIdx.x / N, row = mine < rows ? mine : rows - 1;
+    const bool here = mine < rows;                          // behind the last row the last again, not written
     const T* px = x + row * x_stride;
     const T* pr = residual + row * residual_stride;
     Chunk<T> a[V], b[V];
@@ -182,8 +216,8 @@ __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x,
     for (int v = 0; v < V; ++v) {
         const int c = (v * N + t) * 8;
         if (c + 8 <= channels) {
-            a[v].load(px + c);
-            if (residual) b[v].load(pr + c);
+            a[v].template load<STREAM>(px + c);
+            if (residual) b[v].template load<STREAM>(pr + c);
         } else if (c < channels) {
             load_tail(a[v], px + c, channels - c);
             if (residual) load_tail(b[v], pr + c, channels - c);
@@ -199,7 +233,7 @@ __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x,
             if (residual) h[v][e] += b[v].get(e);
             squares = fmaf(h[v][e], h[v][e], squares);
         }
-        if (sum && c < channels) {
+        if (sum && here && c < channels) {
             T* ps = sum + row * sum_stride + c;
             if (c + 8 <= channels) store8(ps, h[v]);
             else {
@@ -212,13 +246,14 @@ __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x,
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) squares += __shfl_xor(squares, o, 64);
     if constexpr (N > 64) {
-        __shared__ float part[N / 64];
-        if ((t & 63) == 0) part[t >> 6] = squares;
+        __shared__ float part[R][N / 64];
+        if ((t & 63) == 0) part[threadIdx.x / N][t >> 6] = squares;
         __syncthreads();
         squares = 0.f;
 #pragma unroll
-        for (int w = 0; w < N / 64; ++w) squares += part[w];
+        for (int w = 0; w < N / 64; ++w) squares += part[threadIdx.x / N][w];
     }
+    if (!here) return;
     const float inv = rsqrtf(squares / (float)channels + eps);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -235,16 +270,17 @@ __global__ __launch_bounds__(N < 256 ? 256 : N) void rms_norm_kernel(const T* x,
         for (int e = 0; e < 8; ++e) y[e] = c + e < channels ? y[e] : 0.f;
         const float s = scale_of(max16(magnitude(y)));
         if ((t & 15) == 0) scale[(long long)(c / kBlock) * scale_stride + row] = s;
-        store_q(q + row * q_stride + c, y, 1.f / s, channels - c);
+        store_q(q + row * q_stride + c, y, inverse(s), channels - c);
     }
 }
 
 hipError_t launch_rms_norm_fp8(const RowsFp8& a, const NormFp8& n, bool bf16, hipStream_t stream)
 {
+    const bool stream_in = (long long)a.rows * a.channels * (n.residual ? 2 : 1) * (bf16 ? 2 : 4) > kStreamBytes;
     auto go = [&](auto type, auto threads, auto chunks) {
         typedef decltype(type) T;
         constexpr int N = threads(), V = chunks(), R = N < 256 ? 256 / N : 1;
-        hipLaunchKernelGGL((rms_norm_kernel<T, N, V>), dim3((unsigned)((a.rows - 1) / R + 1)), dim3(N < 256 ? 256 : N), 0, stream,
+        hipLaunchKernelGGL((stream_in ? rms_norm_kernel<T, N, V, true> : rms_norm_kernel<T, N, V, false>), dim3((unsigned)((a.rows - 1) / R + 1)), dim3(N < 256 ? 256 : N), 0, stream,
                            (const T*)n.x, n.x_stride, (const T*)n.residual, n.residual_stride, n.weight, a.rows, a.channels, n.eps,
                            (T*)n.sum, n.sum_stride, a.q, a.q_stride, a.scale, a.scale_stride);
     };
@@ -253,7 +289,7 @@ hipError_t launch_rms_norm_fp8(const RowsFp8& a, const NormFp8& n, bool bf16, hi
         const int c = a.channels;
         if (c <= 512) go(type, integral_constant<int, 64>(), integral_constant<int, 1>());
         else if (c <= 1024) go(type, integral_constant<int, 64>(), integral_constant<int, 2>());
-        else if (c <= 2048) go(type, integral_constant<int, 64>(), integral_constant<int, 4>());
+        else if (c <= 2048) go(type, integral_constant<int, 128>(), integral_constant<int, 2>());
         else if (c <= 4096) go(type, integral_constant<int, 256>(), integral_constant<int, 2>());
         else if (c <= 8192) go(type, integral_constant<int, 256>(), integral_constant<int, 4>());
         else if (c <= 16384) go(type, integral_constant<int, 1024>(), integral_constant<int, 2>());
@@ -301,7 +337,7 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restri
     if (c >= k) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (const int row = row0 + 16 * i; row < n) store_q(q + row * q_stride + c, y[i], 1.f / s, k - c);
+        if (const int row = row0 + 16 * i; row < n) store_q(q + row * q_stride + c, y[i], inverse(s), k - c);
 }
 
 hipError_t launch_quantize_weights_fp8(const void* w, long long w_stride, int n, int k, bool bf16, uint8_t* q, long long q_stride, float* scale,
