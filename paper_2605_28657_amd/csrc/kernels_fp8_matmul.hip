@@ -210,11 +210,15 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 // Piece c of a row is at c ^ key of its row, with keys that are all different in 8 rows whose same piece 8 lanes read together, so that
 // they read all banks once.  MFMA rows stand for weight rows such that a lane's results of two MFMAs are 8 outputs that follow each other: rows
 // 4 g .. 4 g + 3 of MFMAs 2 t and 2 t + 1 are weight rows 32 t + 8 g .. + 7.
+// KS groups of WN x WM waves take the blocks of K in turn, each with panels of its own, and join their sums at the end: two, where the GPU has no second workgroup for a CU
+// that could fill the waits of the first (1500 x 2048 x 5632 by 192 tiles of 128 x 128 28.7 -> 25.0 us, 64 x 11264 x 2048 by 64 x 64 8.5 -> 7.5; where it has one,
+// 1500 x 11264 x 2048, 46 -> 58).
 // DIRECT: the pieces go from memory to LDS without registers, a wave's request is 8 rows (operands at 16-byte addresses); else through registers,
 // at any alignment.  The block that K ends in always goes through registers, with zeros behind K.
-template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJob {
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> struct TileJob {
     static constexpr int W = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM, LN = BN / 8 / W, LM = BM / 8 / W, T = FN * FM;
-    static constexpr int LDS_BYTES = (3 * BN + 2 * BM) * kBlock;
+    static constexpr int GROUP_BYTES = (3 * BN + 2 * BM) * kBlock, LDS_BYTES = KS * GROUP_BYTES;
+    static_assert(KS == 1 || KS * BN * BM * 4 <= LDS_BYTES, "the groups' sums are joined where their panels were");
     static constexpr int GAP = 3 * (LN + LM) <= T ? 3 : 2 * (LN + LM) <= T ? 2 : 1;   // a request every GAP MFMAs
     static constexpr int FREE_A = GAP * LN > FM ? GAP * LN : FM;     // every wave has its rows in registers: before this MFMA their panel is free
     static_assert(BN % (8 * W) == 0 && BM % (8 * W) == 0 && kBlock % (16 * FN) == 0 && FN % 2 == 0 && W % 2 == 0, "");
@@ -222,7 +226,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
 
     const MatmulFp8& a;
     uint8_t* lds;
-    const int lane, wave, col, piece, wn, wm, blocks, whole;
+    const int lane, group, wave, col, piece, wn, wm, blocks, whole;   // wave: in its group
     // a lane's piece in the wave's requests and its rows' offsets; of the rows behind the last one the last again, not stored
     const int src_w, src_a, at_w, at_a;
     int last_w, last_a;
@@ -240,7 +244,8 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
     static __device__ __forceinline__ int row_w(int col) { return (col >> 2) * 8 + (col & 3); }
 
     __device__ __forceinline__ TileJob(const MatmulFp8& args, uint8_t* shared)
-        : a(args), lds(shared), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), col(lane & 15), piece(lane >> 4),
+        : a(args), lds(shared + __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)) * GROUP_BYTES), lane(threadIdx.x & 63),
+          group(__builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W))), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % W), col(lane & 15), piece(lane >> 4),
           wn(wave % WN), wm(wave / WN), blocks((args.k + kBlock - 1) / kBlock), whole(args.k / kBlock),
           src_w((lane & 7) ^ key_w(wave * 8 + (lane >> 3))), src_a((lane & 7) ^ (lane >> 3)),
           at_w(row_w(col) * kBlock + (piece ^ key_w(row_w(col))) * 16), at_a(col * kBlock + (piece ^ (col & 7)) * 16) {}
@@ -303,14 +308,14 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
     // requests the first two blocks; nobody reads LDS
     __device__ __forceinline__ void prime()
     {
-        load_scales(0);
         if (whole > 0) {
+            load_scales(min(group, whole - 1));
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                for (int l = 0; l < LN; ++l) bring_w(l, min(b, whole - 1), panel_w(b));
+                for (int l = 0; l < LN; ++l) bring_w(l, min(b * KS + group, whole - 1), panel_w(b));
 #pragma unroll
-                for (int l = 0; l < LM; ++l) bring_a(l, min(b, whole - 1), panel_a(b));
+                for (int l = 0; l < LM; ++l) bring_a(l, min(b * KS + group, whole - 1), panel_a(b));
                 put(panel_w(b), panel_a(b));
             }
         }
@@ -366,17 +371,22 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
     __device__ __forceinline__ void multiply()
     {
         clear();
-        next_scales();
-        int now = 0;                                         // the panel of weights of block b, b % 3
-        for (int b = 0; b < whole; ++b) {
+        if (whole > 0) next_scales();
+        int now = 0;                                         // the panel of weights of the group's block i, i % 3
+        for (int i = 0; i * KS < whole; ++i) {
             // the block has landed (the next one's requests may be on their way), and nobody reads the panel of weights of the block before
             if (DIRECT) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
             else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            load_scales(min(b + 1, blocks - 1));
+            // past the last whole block the last one again: with a branch the compiler could not count the requests
+            load_scales(min((i + 1) * KS + group, whole - 1));
             __builtin_amdgcn_sched_barrier(0);
-            uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(b & 1);
-            // past the last whole block the last one again, which nothing reads: with a branch the compiler could not count the requests
-            block<true>(panel_w(now), to_a, min(b + 2, whole - 1), to_w, to_a);
+            if (KS > 1 && i * KS + group >= whole) {
+                // a group without a block in the last turn takes the last one with a scale of zero: where that is NaN the result is NaN without it, too
+#pragma unroll
+                for (int j = 0; j < FM; ++j) s[j] = 0.f;
+            }
+            uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(i & 1);
+            block<true>(panel_w(now), to_a, min((i + 2) * KS + group, whole - 1), to_w, to_a);
             put(to_w, to_a);
             next_scales();
             now = now == 2 ? 0 : now + 1;
@@ -384,17 +394,48 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
         // the surplus requests have landed before LDS is written again or given back
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (whole < blocks) {
+            if (group == 0) {
+                load_scales(whole);
 #pragma unroll 1
-            for (int g = wave; g < (BN + BM) / 8; g += W) {
-                const bool of_w = g < BN / 8;
-                const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
-                const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
-                *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
+                for (int g = wave; g < (BN + BM) / 8; g += W) {
+                    const bool of_w = g < BN / 8;
+                    const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
+                    const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
+                    *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
+                }
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            block<false>(panel_w(0), panel_a(0), 0, lds, lds);
+            if (group == 0) {
+                next_scales();
+                block<false>(panel_w(0), panel_a(0), 0, lds, lds);
+            }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         }
+        if constexpr (KS > 1) join();
+    }
+
+    // KS > 1: a cell, a lane's 8 outputs that follow each other, gets the other groups' sums in the group that stores it
+    __device__ __forceinline__ bool owns(int i, int j) { return KS == 1 || (i / 2 * FM + j) % KS == group; }
+    __device__ __forceinline__ void join()
+    {
+        f32x4* sums = reinterpret_cast<f32x4*>(lds - group * GROUP_BYTES);
+        auto at = [&](int g, int i, int j) __attribute__((always_inline)) { return ((g * FN + i) * FM + j) * (64 * W) + wave * 64 + lane; };
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                if (!owns(i, j)) sums[at(group, i, j)] = acc[i][j];
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+                if (owns(i, j)) {
+                    f32x4 v = group == 0 ? acc[i][j] : sums[at(0, i, j)];
+#pragma unroll
+                    for (int g = 1; g < KS; ++g) v += g == group ? acc[i][j] : sums[at(g, i, j)];
+                    acc[i][j] = v;
+                }
     }
 
     // The same where K is two whole blocks or more and another tile, at (n1, m1), follows: its first two blocks are requested in this one's last two.
@@ -433,6 +474,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT> struct TileJo
             }
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
+                if (!owns(i, j)) continue;
                 const int m = m0 + (wm * FM + j) * 16 + col;
                 float v[8];
 #pragma unroll
@@ -452,10 +494,10 @@ __device__ __forceinline__ void place(int tile, int tiles_n, int tiles_m, int& a
     at_m = strip * 8 + in_strip % high;
 }
 
-template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU>
-__global__ __launch_bounds__(64 * WN * WM, EU) void matmul_tile_kernel(MatmulFp8 a)
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU, int KS = 1>
+__global__ __launch_bounds__(64 * WN * WM * KS, EU) void matmul_tile_kernel(MatmulFp8 a)
 {
-    typedef TileJob<O, WN, WM, FN, FM, DIRECT> Job;
+    typedef TileJob<O, WN, WM, FN, FM, DIRECT, KS> Job;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[Job::LDS_BYTES];
     // workgroups go round the 8 XCDs: each XCD takes tiles that follow each other
     const int tiles_n = (a.n + Job::BN - 1) / Job::BN, tiles_m = (a.rows + Job::BM - 1) / Job::BM, tiles = tiles_n * tiles_m, xcd = blockIdx.x & 7;
@@ -515,11 +557,11 @@ template <bool BIAS> __global__ __launch_bounds__(512, 2) void matmul_rounds_ker
     }
 }
 
-template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU> static hipError_t launch_tile(const MatmulFp8& a, hipStream_t stream)
+template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU, int KS = 1> static hipError_t launch_tile(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 16 * FN * WN - 1) / (16 * FN * WN)) * ((a.rows + 16 * FM * WM - 1) / (16 * FM * WM));
     if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU>), dim3((unsigned)tiles), dim3(64 * WN * WM), 0, stream, a);
+    hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU, KS>), dim3((unsigned)tiles), dim3(64 * WN * WM * KS), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -542,19 +584,20 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 // What a block of K of one tile takes on a GPU that is full of such tiles, in ns (8192 x 8192 x 8192 and, for fp32 and for operands at any address,
 // 4096 x 4096 x 4096).  A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU
 // decide it: 12000 x 11264 x 2048 in us by 256 x 256 in rounds 258, a workgroup a tile 287, 128 x 128 318, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 43, 58, 47, 53, 61;
-// 1500 x 2048 x 5632 -, 59, 26.7, 28.5, 30; 300 x 11264 x 2048 -, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 -, 25.5, 12.3, 9.4, 8.7.
+// 1500 x 2048 x 5632 33, 59, 25, 28.5, 30; 300 x 11264 x 2048 28, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 12.5, 25.5, 11.8, 8.5, 7.5.
 struct TileCost { int n, m, ns; };
+struct Choice { int tile; bool alone; };                     // alone: a CU has at most one of the tiles
 
-static int cheapest(const MatmulFp8& a, const TileCost* tiles, int count, bool first_in_rounds)
+static Choice cheapest(const MatmulFp8& a, const TileCost* tiles, int count, bool first_in_rounds)
 {
-    int best = 0;
+    Choice best = {0, false};
     long long least = 0;
     for (int i = 0; i < count; ++i) {
         const long long all = (long long)((a.n + tiles[i].n - 1) / tiles[i].n) * ((a.rows + tiles[i].m - 1) / tiles[i].m);
         long long cost = (all + 255) / 256 * tiles[i].ns;
         // matmul_rounds_kernel: a last round of up to 8 tiles an XCD takes two fifths of a round
         if (const long long left = (all + 7) / 8 % 32; i == 0 && first_in_rounds && left > 0 && left <= 8) cost -= tiles[i].ns * 3 / 5;
-        if (i == 0 || cost < least) { best = i; least = cost; }
+        if (i == 0 || cost < least) { best = {i, all <= 256}; least = cost; }
     }
     return best;
 }
@@ -563,16 +606,17 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 640}};
-        if (cheapest(a, tiles, 2, false) == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
     }
     static constexpr TileCost tiles[] = {{256, 256, 1750}, {128, 128, 550}, {128, 64, 340}, {64, 64, 213}};
     const bool rounds = a.k % kBlock == 0 && a.k >= 2 * kBlock;
-    switch (cheapest(a, tiles, 4, rounds)) {
+    const Choice c = cheapest(a, tiles, 4, rounds);
+    switch (c.tile) {
     case 0: return rounds ? launch_rounds(a, stream) : launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
-    case 1: return launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
-    case 2: return launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
-    default: return launch_tile<uint16_t, 2, 2, 2, 2, true, 4>(a, stream);
+    case 1: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
+    case 2: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
+    default: return c.alone ? launch_tile<uint16_t, 2, 2, 2, 2, true, 4, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 2, 2, true, 4>(a, stream);
     }
 }
 
@@ -580,14 +624,15 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 1220}, {128, 64, 780}};
-        if (cheapest(a, tiles, 2, false) == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
     }
     static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 64, 570}, {64, 64, 305}};
-    switch (cheapest(a, tiles, 3, false)) {
-    case 0: return launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
-    case 1: return launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
-    default: return launch_tile<float, 2, 2, 2, 2, true, 3>(a, stream);
+    const Choice c = cheapest(a, tiles, 3, false);
+    switch (c.tile) {
+    case 0: return c.alone ? launch_tile<float, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
+    case 1: return c.alone ? launch_tile<float, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
+    default: return c.alone ? launch_tile<float, 2, 2, 2, 2, true, 3, 2>(a, stream) : launch_tile<float, 2, 2, 2, 2, true, 3>(a, stream);
     }
 }
 

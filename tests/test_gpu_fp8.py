@@ -445,3 +445,22 @@ def test_product_in_rounds(rows, n, k):
     if rows % 5 == 0:
         latent = pa.matmul_fp8(a, sa, w, sw, n_frames=rows // 5)
         assert torch.equal(latent, want.bfloat16().view(5, rows // 5, n).transpose(1, 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,k", [(300, 600, 128), (300, 600, 256), (300, 600, 384), (300, 600, 400), (1300, 2000, 656), (1400, 1900, 1152), (500, 2100, 512), (150, 4000, 1040),
+                                      (40, 8200, 384), (70, 8200, 2064), (700, 700, 127)])
+def test_product_of_few_tiles_with_k_in_two_groups(rows, n, k, dtype):
+    """One block of K, odd numbers of them, and a block that K ends in, where two groups of waves take the blocks in turn."""
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+    want = (a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()
+    aligned = -(-k // 16) * 16
+    got = pa.matmul_fp8(laid_out(a, aligned), sa, laid_out(w, aligned), sw, dtype=TORCH[dtype])
+    assert torch.equal(got, want.to(TORCH[dtype]))
+    bad = a.clone()
+    bad.view(torch.uint8)[5, k - 1] = 0x7f
+    got = pa.matmul_fp8(laid_out(bad, aligned), sa, laid_out(w, aligned), sw, dtype=TORCH[dtype])
+    assert bool(torch.isnan(got[5]).all()) and int(torch.isnan(got).sum()) == n and torch.equal(got[6:], want[6:].to(TORCH[dtype]))
