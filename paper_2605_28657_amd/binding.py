@@ -326,6 +326,7 @@ def _launch(fn, device, *args):
     """fn(*args, stream) on the current stream of `device`, with that device current."""
     import torch
     index = device.index
+    assert device.type == "cuda"
     if index == torch.cuda.current_device():
         # the stream's address as it is, without the Stream object around it (1.7 us of a call)
         status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
@@ -339,7 +340,7 @@ def _launch(fn, device, *args):
 def _matrix(t, dtype, device) -> int:
     """The row stride of a matrix on `device` whose channels follow each other (a slice of a wider matrix is fine)."""
     stride = t.stride()
-    assert t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or t.shape[1] == 1) and t.device == device and device.type == "cuda"
+    assert t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or t.shape[1] == 1) and t.device == device
     return stride[0]
 
 
@@ -409,14 +410,15 @@ def rms_norm_fp8(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=
         rs = _matrix(residual, xt, device)
         assert residual.shape == shape
         rp = residual.data_ptr()
-        if sum_out is None:
-            sum_out = x.new_empty(shape)
     if sum_out is not None:
         hs = _apart(_matrix(sum_out, xt, device), channels, rows)
         assert sum_out.shape == shape
         hp = sum_out.data_ptr()
         if rows == 1:                       # a single row's stride says nothing
             xs = rs = hs
+    elif residual is not None:
+        sum_out, hs = x.new_empty(shape), channels
+        hp = sum_out.data_ptr()
     q, qs, scale, ss = _fp8_rows(x, rows, channels, out)
     _launch(load_library().demon_vae_rms_norm_fp8, device, xp, xs, rp, rs, weight.data_ptr(), rows, channels, eps, dtype, hp, hs,
             q.data_ptr(), qs, scale.data_ptr(), ss)
@@ -458,13 +460,10 @@ def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0,
     assert n_frames >= 0 and (n_frames == 0 or rows % n_frames == 0)
     shape = (rows // n_frames, n, n_frames) if n_frames else (rows, n)
     if out is None:
-        out = a.new_empty(shape, dtype=dtype or torch.bfloat16)
-    assert out.shape == shape and out.device == device and dtype in (None, out.dtype)
-    if n_frames:
-        assert out.is_contiguous()
-        os_ = 0
+        out, os_ = a.new_empty(shape, dtype=dtype or torch.bfloat16), n
     else:
-        os_ = _apart(_matrix(out, out.dtype, device), n, rows)
+        assert out.shape == shape and out.device == device and (dtype is None or dtype is out.dtype) and (n_frames == 0 or out.is_contiguous())
+        os_ = 0 if n_frames else _apart(_matrix(out, out.dtype, device), n, rows)
     _launch(load_library().demon_vae_matmul_fp8, device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
             w_scale.data_ptr(), 0 if bias is None else bias.data_ptr(), rows, n, k, n_frames, _demon_dtype(out.dtype), out.data_ptr(), os_)
     return out
