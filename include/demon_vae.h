@@ -365,7 +365,7 @@ DEMON_API demon_status demon_vae_crossfade(const float* d_prev_tail, long long p
  *   d_x     : device, [rows][channels] or [rows][2 channels], fp32 (DEMON_F32) or bf16 (DEMON_BF16), rows x_stride elements apart
  *   d_q     : device, e4m3 [rows][channels], rows q_stride bytes apart
  *   d_scale : device, fp32 [ceil(channels / 128)][rows], blocks scale_stride floats apart
- * UNSUPPORTED: channels > 16777216.
+ * UNSUPPORTED: channels > 16777216, rows > 4194303.
  */
 DEMON_API demon_status demon_vae_quantize_fp8(const void* d_x, long long x_stride, int rows, int channels, int gated, demon_dtype dtype,
                                               void* d_q, long long q_stride, float* d_scale, long long scale_stride, void* stream);
@@ -378,7 +378,7 @@ DEMON_API demon_status demon_vae_quantize_fp8(const void* d_x, long long x_strid
  *   d_weight        : device, fp32 [channels]
  *   d_sum           : device, h in the type of d_x, or NULL.  May be d_x or d_residual itself (same pointer and stride)
  *   d_q, d_scale    : as for demon_vae_quantize_fp8
- * INVALID_ARG also for eps negative, infinite or NaN.  UNSUPPORTED: channels > 32768.
+ * INVALID_ARG also for eps negative, infinite or NaN.  UNSUPPORTED: channels > 32768, rows > 4194303.
  */
 DEMON_API demon_status demon_vae_rms_norm_fp8(const void* d_x, long long x_stride, const void* d_residual, long long residual_stride,
                                               const float* d_weight, int rows, int channels, float eps, demon_dtype dtype,
@@ -387,7 +387,7 @@ DEMON_API demon_status demon_vae_rms_norm_fp8(const void* d_x, long long x_strid
 
 /*
  * A weight matrix [n][k] (fp32 or bf16, rows w_stride elements apart) in 8 bits: d_q e4m3 [n][k], rows q_stride bytes apart, and
- * d_scale fp32 [ceil(n / 128)][ceil(k / 128)], without gaps.  UNSUPPORTED: n or k > 16777216, more than 2^31 - 1 blocks.
+ * d_scale fp32 [ceil(n / 128)][ceil(k / 128)], without gaps.  UNSUPPORTED: n or k > 16777216, 16777216 blocks or more.
  */
 DEMON_API demon_status demon_vae_quantize_weights_fp8(const void* d_w, long long w_stride, int n, int k, demon_dtype dtype,
                                                       void* d_q, long long q_stride, float* d_scale, void* stream);

@@ -20,6 +20,7 @@ demon_status check_rows(int rows, int channels, demon_dtype dtype, const void* q
     if (dtype != DEMON_F32 && dtype != DEMON_BF16) return fail(DEMON_ERR_INVALID_ARG, "unknown dtype");
     if (q_stride < channels) return fail(DEMON_ERR_INVALID_ARG, "8-bit rows overlap");
     if (scale_stride < rows) return fail(DEMON_ERR_INVALID_ARG, "scales of blocks overlap");
+    if (rows > kFp8Rows) return fail(DEMON_ERR_UNSUPPORTED, "more than %d rows", kFp8Rows);
     return DEMON_OK;
 }
 
@@ -66,7 +67,7 @@ demon_status demon_vae_quantize_weights_fp8(const void* d_w, long long w_stride,
     if (dtype != DEMON_F32 && dtype != DEMON_BF16) return fail(DEMON_ERR_INVALID_ARG, "unknown dtype");
     if (w_stride < 0) return fail(DEMON_ERR_INVALID_ARG, "negative row stride");
     if (q_stride < k) return fail(DEMON_ERR_INVALID_ARG, "8-bit rows overlap");
-    if (n > (1 << 24) || k > (1 << 24) || (long long)blocks_of(n) * blocks_of(k) > 0x7fffffffll) return fail(DEMON_ERR_UNSUPPORTED, "matrix too large");
+    if (n > (1 << 24) || k > (1 << 24) || (long long)blocks_of(n) * blocks_of(k) >= (1 << 24)) return fail(DEMON_ERR_UNSUPPORTED, "matrix too large");
     return launched(launch_quantize_weights_fp8(d_w, w_stride, n, k, dtype == DEMON_BF16, (uint8_t*)d_q, q_stride, d_scale, (hipStream_t)stream),
                     "quantize weights");
 }

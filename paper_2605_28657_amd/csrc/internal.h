@@ -211,6 +211,7 @@ hipError_t launch_quantize_fp8(const RowsFp8& a, const void* x, long long x_stri
 struct NormFp8 { const void* x; long long x_stride; const void* residual; long long residual_stride; const float* weight; float eps;
                  void* sum; long long sum_stride; };
 constexpr int kNormFp8Channels = 32768;      // a row is held in the registers of at most 1024 threads
+constexpr int kFp8Rows = (1 << 22) - 1;      // of rows that are written in 8 bits: a launch has at most 2^32 - 1 threads
 hipError_t launch_rms_norm_fp8(const RowsFp8& a, const NormFp8& n, bool bf16, hipStream_t stream);
 // weights [n][k] in e4m3 with the scales [blocks of 128 rows][blocks of 128 columns]
 hipError_t launch_quantize_weights_fp8(const void* w, long long w_stride, int n, int k, bool bf16, uint8_t* q, long long q_stride, float* scale,

@@ -344,7 +344,6 @@ hipError_t launch_quantize_weights_fp8(const void* w, long long w_stride, int n,
                                        hipStream_t stream)
 {
     const long long blocks = (long long)((n + kBlock - 1) / kBlock) * ((k + kBlock - 1) / kBlock);
-    if (blocks > 0x7fffffffll) return hipErrorInvalidValue;
     if (bf16) hipLaunchKernelGGL(quantize_weights_kernel<uint16_t>, dim3((unsigned)blocks), dim3(256), 0, stream, (const uint16_t*)w, w_stride, n, k, q, q_stride, scale);
     else hipLaunchKernelGGL(quantize_weights_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, stream, (const float*)w, w_stride, n, k, q, q_stride, scale);
     return hipGetLastError();

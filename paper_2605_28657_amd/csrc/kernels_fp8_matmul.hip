@@ -85,6 +85,9 @@ __device__ __forceinline__ void request16(__amdgpu_buffer_rsrc_t rs, uint8_t* to
 __device__ __forceinline__ void store_out(uint16_t* p, float v) { *p = f32_to_bf16_bits(v); }
 __device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
 
+// A launch has at most 2^32 - 1 threads.
+inline bool fits(long long workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
 // Where out[m][n] is: rows of n values, or the latent [clip][n][frame] of rows m = clip * n_frames + frame.
 template <typename O> __device__ __forceinline__ O* out_at(const MatmulFp8& a, long long m, long long n)
 {
@@ -560,7 +563,7 @@ template <bool BIAS> __global__ __launch_bounds__(512, 2) void matmul_rounds_ker
 template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU, int KS = 1> static hipError_t launch_tile(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 16 * FN * WN - 1) / (16 * FN * WN)) * ((a.rows + 16 * FM * WM - 1) / (16 * FM * WM));
-    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    if (!fits(tiles, 64 * WN * WM * KS)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU, KS>), dim3((unsigned)tiles), dim3(64 * WN * WM * KS), 0, stream, a);
     return hipGetLastError();
 }
@@ -576,7 +579,7 @@ static hipError_t launch_rounds(const MatmulFp8& a, hipStream_t stream)
 template <typename O, int FN, int FM, int W, int U> static hipError_t launch_direct(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 16 * FN - 1) / (16 * FN)) * ((a.rows + 16 * FM - 1) / (16 * FM));
-    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    if (!fits(tiles, 64 * W)) return hipErrorInvalidValue;
     hipLaunchKernelGGL((matmul_direct_kernel<O, FN, FM, W, U>), dim3((unsigned)tiles), dim3(64 * W), 0, stream, a);
     return hipGetLastError();
 }

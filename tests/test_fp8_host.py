@@ -29,7 +29,7 @@ MATMUL = dict(a=P, a_stride=256, a_scale=P, a_scale_stride=4, w=P, w_stride=256,
 @pytest.mark.parametrize("change,status", [
     (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(rows=0), INVALID), (dict(rows=-1), INVALID),
     (dict(channels=0), INVALID), (dict(dtype=2), INVALID), (dict(dtype=-1), INVALID), (dict(x_stride=-1), INVALID), (dict(q_stride=255), INVALID),
-    (dict(scale_stride=3), INVALID), (dict(channels=(1 << 24) + 1, q_stride=1 << 25), UNSUPPORTED)])
+    (dict(scale_stride=3), INVALID), (dict(channels=(1 << 24) + 1, q_stride=1 << 25), UNSUPPORTED), (dict(rows=1 << 22, scale_stride=1 << 22), UNSUPPORTED)])
 def test_quantize_refuses(change, status):
     rc, message = _call("demon_vae_quantize_fp8", QUANTIZE, change)
     assert rc == status and message
@@ -42,7 +42,7 @@ def test_quantize_refuses(change, status):
     (dict(x_stride=512), INVALID),                                      # sum in place of x with another stride
     (dict(x=ctypes.c_void_p(8192), residual_stride=512), INVALID),      # the same for the residual
     (dict(q_stride=1), INVALID), (dict(scale_stride=0), INVALID),
-    (dict(channels=32769, x_stride=32769, residual_stride=32769, sum_stride=32769, q_stride=32769), UNSUPPORTED)])
+    (dict(rows=1 << 22, scale_stride=1 << 22), UNSUPPORTED), (dict(channels=32769, x_stride=32769, residual_stride=32769, sum_stride=32769, q_stride=32769), UNSUPPORTED)])
 def test_norm_refuses(change, status):
     rc, message = _call("demon_vae_rms_norm_fp8", NORM, change)
     assert rc == status and message
@@ -51,7 +51,7 @@ def test_norm_refuses(change, status):
 @pytest.mark.parametrize("change,status", [
     (dict(w=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID), (dict(n=0), INVALID), (dict(k=0), INVALID), (dict(dtype=2), INVALID),
     (dict(w_stride=-1), INVALID), (dict(q_stride=255), INVALID), (dict(n=(1 << 24) + 1), UNSUPPORTED),
-    (dict(n=1 << 24, k=1 << 24, q_stride=1 << 24), UNSUPPORTED)])
+    (dict(n=1 << 24, k=1 << 24, q_stride=1 << 24), UNSUPPORTED), (dict(n=1 << 19, k=1 << 19, q_stride=1 << 19), UNSUPPORTED)])
 def test_weights_refuse(change, status):
     rc, message = _call("demon_vae_quantize_weights_fp8", WEIGHTS, change)
     assert rc == status and message
@@ -82,3 +82,11 @@ def test_tensors_that_are_not_on_a_gpu_are_refused():
         pa.matmul_fp8(q, s, q, torch.zeros(1, 2))
     with pytest.raises(KeyError):
         pa.quantize_fp8(x.half())
+
+
+def test_kernels_keep_their_sums_in_registers():
+    """Sums and operands of the products live in registers; in scratch memory they would make a round trip in every block of K."""
+    from test_kernel_sources import _resources
+    res = {n: r for n, r in _resources().items() if "matmul_" in n or "rms_norm_kernel" in n or "quantize_" in n}
+    assert len(res) > 40
+    assert {n: r for n, r in res.items() if r != (0, 0)} == {}

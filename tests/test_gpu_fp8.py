@@ -184,7 +184,7 @@ def test_weights_of_special_values():
 # ---------------------------------------------------------------------------------- matrix product
 SIZES = [(1, 1, 1), (1, 64, 128), (2, 17, 16), (7, 65, 129), (16, 128, 256), (17, 130, 1111), (1, 2048, 2048), (8, 1000, 640), (33, 96, 4096),
          (64, 64, 127), (65, 64, 15), (75, 192, 320), (128, 128, 128), (129, 257, 384), (300, 520, 1040), (513, 300, 2000), (700, 1030, 528), (2100, 260, 136),
-         (1500, 64, 1111), (260, 2100, 96)]
+         (1500, 64, 1111), (260, 2100, 96), (2300, 2100, 272)]
 
 
 def _operands(rows, n, k, seed=0):
@@ -427,14 +427,15 @@ def test_wrong_tensors_are_refused():
         pa.matmul_fp8(a, sa, w, sw, out=torch.zeros(64, device=DEV).as_strided((4, 8), (4, 1)))
 
 
-# tiles in rounds (K a multiple of 128 from 256 on, many tiles): a last round cut in parts or not, ragged edges, K of 2, 3 and more blocks
-@pytest.mark.parametrize("rows,n,k", [(4096, 4096, 256), (4100, 4090, 384), (4097, 4352, 256), (5000, 6200, 512), (2050, 8200, 640), (8200, 8200, 256)])
-def test_product_in_rounds(rows, n, k):
+# 256 x 256 tiles, in rounds where K is a multiple of 128 from 256 on: a last round cut in parts or not, ragged edges, K of 1, 2, 3 and more blocks
+@pytest.mark.parametrize("rows,n,k", [(4096, 4096, 100), (4096, 4096, 128), (4100, 4090, 136), (4096, 4096, 400), (4096, 4096, 256), (4100, 4090, 384), (4097, 4352, 256), (5000, 6200, 512), (2050, 8200, 640), (8200, 8200, 256)])
+def test_product_of_many_tiles(rows, n, k):
     g = torch.Generator().manual_seed(rows + n + k)
     whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
     powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
     for again in range(2):
-        a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+        aligned = -(-k // 16) * 16
+        a, w, sa, sw = laid_out(whole(rows, k), aligned), laid_out(whole(n, k), aligned), powers(blocks(k), rows), powers(blocks(n), blocks(k))
         bias = torch.randint(-9, 10, (n,), generator=g).float().to(DEV)
         # whole numbers of quarters below 2^24: fp32 has them exactly, and so has a product of fp32 matrices
         want = (a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()
