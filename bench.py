@@ -30,13 +30,14 @@ def grid_of(handle):
 
 
 def kernel_sources_digest():
-    """Digest of the library's device code, without comments and white space: what a counter profile was taken of."""
+    """Digest of the device code that decodes and encodes run (the sources of the operators in 8 bits are not among it), without comments and white
+    space: what a counter profile was taken of."""
     import glob
     import hashlib
     import re
     h = hashlib.sha256()
     for path in sorted(glob.glob(os.path.join(ROOT, "paper_2605_28657_amd", "csrc", "*"))):
-        if path.endswith((".hip", ".h", ".cpp")) and not path.endswith("mfma_probe.hip"):
+        if path.endswith((".hip", ".h", ".cpp")) and not path.endswith("mfma_probe.hip") and "fp8" not in os.path.basename(path):
             text = re.sub(r"//[^\n]*|/\*.*?\*/", "", open(path).read(), flags=re.S)
             h.update(os.path.basename(path).encode() + re.sub(r"\s+", "", text).encode())
     return h.hexdigest()[:16]

@@ -1,5 +1,5 @@
 // C entry points of the operands in 8 bits and of their product: argument checks, then one launch each.
-#include "internal.h"
+#include "fp8.h"
 
 using namespace demon;
 

@@ -13,7 +13,10 @@
 // A thread holds 8 channels that follow each other (16 bytes of bf16, 32 of fp32), so that a block is 16 lanes, the row of the wave's
 // cross-lane moves: its maximum needs no LDS.  Loads and stores of whole chunks take any alignment that the type has (the hardware's 16-byte
 // loads do); the chunk that the row ends in is read and written by elements.
+#include <type_traits>
+
 #include "device_common.h"
+#include "fp8.h"
 
 namespace demon {
 

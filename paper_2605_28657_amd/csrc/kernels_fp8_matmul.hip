@@ -15,7 +15,10 @@
 // Operand layout: lane l of either operand holds row l % 16 of its tile and, of a block of 128 values of K, the pieces of 16 bytes
 // l / 16 and l / 16 + 4.  Which values of K a lane holds is free as long as A and B agree, since the MFMA sums over all of them; with these
 // pieces one load of a wave reads 64 bytes that follow each other of each of 16 rows.
+#include <type_traits>
+
 #include "device_common.h"
+#include "fp8.h"
 
 namespace demon {
 
