@@ -66,15 +66,30 @@ __device__ __forceinline__ f32x4 block_product(const Operand<float>& a, const Op
     return p;
 }
 
-// A piece of 16 values at p, of which the first `left` belong to the row; zeros for the others, which are not read.
-__device__ __forceinline__ u32x4 load_piece(const uint8_t* p, int left)
+// The 16 bytes without the first `missing` (0 .. 15), zeros behind the last.
+__device__ __forceinline__ u32x4 shifted(u32x4 v, int missing)
+{
+    const uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+    const int bits = 8 * missing;
+    const uint64_t new_lo = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : hi >> (bits - 64), new_hi = bits < 64 ? hi >> bits : 0;
+    return u32x4{(uint32_t)new_lo, (uint32_t)(new_lo >> 32), (uint32_t)new_hi, (uint32_t)(new_hi >> 32)};
+}
+
+// A piece of 16 values at p, of which the first `left` belong to a row of k values; zeros for the others, which are not read.  The piece that a row of 16 values or
+// more ends in is the row's last 16 bytes, shifted: one load.  (Byte by byte, each behind a branch of its own, it takes 15 one after another: 600 x 2048 x 2047
+// 27.5 us, this 20.7.)
+__device__ __forceinline__ u32x4 load_piece(const uint8_t* p, int left, int k)
 {
     u32x4 v = {};
-    if (left >= 16) v = *reinterpret_cast<const loose16*>(p);
-    else {
+    if (left <= 0) return v;
+    if (k >= 16) {
+        const int missing = left < 16 ? 16 - left : 0;
+        return shifted(*reinterpret_cast<const loose16*>(p - missing), missing);
+    }
 #pragma unroll
-        for (int e = 0; e < 15; ++e)
-            if (e < left) v[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
+    for (int e = 0; e < 15; ++e) {
+        const uint32_t byte = p[e < left ? e : left - 1];
+        v[e / 4] |= (e < left ? byte : 0) << (8 * (e % 4));
     }
     return v;
 }
@@ -188,7 +203,7 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
     int b = wave;
     for (; b + (U - 1) * W < whole; b += U * W) take(std::integral_constant<int, U>(), b, all);
     for (; b < whole; b += W) take(std::integral_constant<int, 1>(), b, all);
-    if (b < blocks) take(std::integral_constant<int, 1>(), b, [&](const uint8_t* p, int behind) __attribute__((always_inline)) { return load_piece(p, left - behind); });
+    if (b < blocks) take(std::integral_constant<int, 1>(), b, [&](const uint8_t* p, int behind) __attribute__((always_inline)) { return load_piece(p, left - behind, a.k); });
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
@@ -210,9 +225,10 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 // ---------------------------------------------------------------------------------- operands through LDS
 // WN x WM waves of 16 FN weight rows by 16 FM rows each.  A panel is a block of K, 128 bytes, of each of the workgroup's weight rows (or rows).  LDS
 // holds three panels of weights and two of rows, and each is requested two blocks ahead: a panel of weights where the one of the block before was,
-// which the barrier at a block's start frees, a panel of rows where the current one is, which a second barrier frees once every wave has it in registers (two buffers
-// each, requested one block ahead at a block's start: 490 us for 8192 x 8192 x 8192, this 439).  The requests are spread over the MFMAs, one for every two:
-// a wave that issues them in a row stands still meanwhile, all waves at once (490 -> 460 us by itself).
+// which the barrier at a block's start frees, a panel of rows where the current one is, which a second barrier frees once every wave has it in registers.  The requests
+// are spread over the MFMAs: a wave that issues them in a row stands still meanwhile, all waves at once.  8192 x 8192 x 8192 by 256 x 256: two buffers of each, requested in
+// a row one block ahead 490 us, spread 460, this 439 to 460 by the board (2390 to 2500 TFLOP/s; the matrix unit is busy for half of its cycles, at the 2.0 to 2.2 GHz that
+// the power limit leaves; without any request the same loop takes 385).
 // Piece c of a row is at c ^ key of its row, with keys that are all different in 8 rows whose same piece 8 lanes read together, so that
 // they read all banks once.  MFMA rows stand for weight rows such that a lane's results of two MFMAs are 8 outputs that follow each other: rows
 // 4 g .. 4 g + 3 of MFMAs 2 t and 2 t + 1 are weight rows 32 t + 8 g .. + 7.
@@ -220,7 +236,8 @@ __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 // that could fill the waits of the first (1500 x 2048 x 5632 by 192 tiles of 128 x 128 28.7 -> 25.0 us, 64 x 11264 x 2048 by 64 x 64 8.5 -> 7.5; where it has one,
 // 1500 x 11264 x 2048, 46 -> 58).
 // DIRECT: the pieces go from memory to LDS without registers, a wave's request is 8 rows (operands at 16-byte addresses); else through registers,
-// at any alignment.  The block that K ends in always goes through registers, with zeros behind K.
+// at any alignment.  `whole` blocks are requested so: those of 128 values and, DIRECT, the one that K ends in where it ends with a piece; else that one goes through
+// registers behind the others, with zeros behind K (12000 x 11264 x 2000 that way 310 us, in rounds 276).
 template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> struct TileJob {
     static constexpr int W = WN * WM, BN = 16 * FN * WN, BM = 16 * FM * WM, LN = BN / 8 / W, LM = BM / 8 / W, T = FN * FM;
     static constexpr int GROUP_BYTES = (3 * BN + 2 * BM) * kBlock, LDS_BYTES = KS * GROUP_BYTES;
@@ -235,11 +252,10 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
     const int lane, group, wave, col, piece, wn, wm, blocks, whole;   // wave: in its group
     // a lane's piece in the wave's requests and its rows' offsets; of the rows behind the last one the last again, not stored
     const int src_w, src_a, at_w, at_a;
-    int last_w, last_a;
     unsigned off_w[LN], off_a[LM];
     const uint8_t *base_w, *base_a;
     __amdgpu_buffer_rsrc_t rs_w, rs_a;
-    u32x4 reg_w[LN], reg_a[LM];                              // !DIRECT: on their way to LDS
+    u32x4 reg_w[LN], reg_a[LM];                              // pieces on their way to LDS that go through registers
     const float* pws;
     unsigned ps[FM];                                         // bytes from a block's scales to a lane's row
     float s[FM], sa[FM], sw;                                 // scales of the current block; of the next one
@@ -252,7 +268,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
     __device__ __forceinline__ TileJob(const MatmulFp8& args, uint8_t* shared)
         : a(args), lds(shared + __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W)) * GROUP_BYTES), lane(threadIdx.x & 63),
           group(__builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W))), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % W), col(lane & 15), piece(lane >> 4),
-          wn(wave % WN), wm(wave / WN), blocks((args.k + kBlock - 1) / kBlock), whole(args.k / kBlock),
+          wn(wave % WN), wm(wave / WN), blocks((args.k + kBlock - 1) / kBlock), whole(DIRECT && args.k % 16 == 0 ? blocks : args.k / kBlock),
           src_w((lane & 7) ^ key_w(wave * 8 + (lane >> 3))), src_a((lane & 7) ^ (lane >> 3)),
           at_w(row_w(col) * kBlock + (piece ^ key_w(row_w(col))) * 16), at_a(col * kBlock + (piece ^ (col & 7)) * 16) {}
 
@@ -266,8 +282,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
         base_a = a.a + (long long)m0 * a.a_stride;
         rs_w = make_rsrc(base_w, 0x7fffffff);
         rs_a = make_rsrc(base_a, 0x7fffffff);
-        last_w = a.n - 1 - n0;
-        last_a = a.rows - 1 - m0;
+        const int last_w = a.n - 1 - n0, last_a = a.rows - 1 - m0;
 #pragma unroll
         for (int l = 0; l < LN; ++l) off_w[l] = (unsigned)(min((l * W + wave) * 8 + (lane >> 3), last_w) * a.w_stride) + src_w * 16;
 #pragma unroll
@@ -280,6 +295,16 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
         for (int j = 0; j < FM; ++j) ps[j] = (unsigned)min(m0 + (wm * FM + j) * 16 + col, a.rows - 1) * 4;
     }
 
+    // Before the requests of block `next`: where K ends in it, pieces behind K are put out of the descriptor's range from here on, and their bytes in LDS become zeros.
+    __device__ __forceinline__ void before(int next)
+    {
+        if (!DIRECT || next != blocks - 1 || a.k % kBlock == 0) return;
+        constexpr unsigned out_of_range = 0xf8000000u;
+#pragma unroll
+        for (int l = 0; l < LN; ++l) off_w[l] = next * kBlock + src_w * 16 < a.k ? off_w[l] : out_of_range;
+#pragma unroll
+        for (int l = 0; l < LM; ++l) off_a[l] = next * kBlock + src_a * 16 < a.k ? off_a[l] : out_of_range;
+    }
     __device__ __forceinline__ void bring_w(int l, int b, uint8_t* to)
     {
         if (DIRECT) request16(rs_w, to + (l * W + wave) * 1024, off_w[l], b * kBlock);
@@ -292,11 +317,43 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
     }
     __device__ __forceinline__ void put(uint8_t* to_w, uint8_t* to_a)
     {
-        if (DIRECT) return;
+        if (!DIRECT) write_panels(to_w, to_a);
+    }
+    __device__ __forceinline__ void write_panels(uint8_t* to_w, uint8_t* to_a)
+    {
 #pragma unroll
         for (int l = 0; l < LN; ++l) *reinterpret_cast<u32x4*>(to_w + (l * W + wave) * 1024 + lane * 16) = reg_w[l];
 #pragma unroll
         for (int l = 0; l < LM; ++l) *reinterpret_cast<u32x4*>(to_a + (l * W + wave) * 1024 + lane * 16) = reg_a[l];
+    }
+    // The block that K ends in, into registers: see load_piece(); all loads before the first shift.
+    __device__ __forceinline__ void fetch_end()
+    {
+        const int at = whole * kBlock, left_w = a.k - at - src_w * 16, left_a = a.k - at - src_a * 16;
+        if (a.k < 16) {
+#pragma unroll
+            for (int l = 0; l < LN; ++l) reg_w[l] = load_piece(base_w + off_w[l], left_w, a.k);
+#pragma unroll
+            for (int l = 0; l < LM; ++l) reg_a[l] = load_piece(base_a + off_a[l], left_a, a.k);
+            return;
+        }
+        const int missing_w = left_w < 16 ? 16 - left_w : 0, missing_a = left_a < 16 ? 16 - left_a : 0;
+#pragma unroll
+        for (int l = 0; l < LN; ++l) reg_w[l] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int l = 0; l < LM; ++l) reg_a[l] = u32x4{0, 0, 0, 0};
+        if (left_w > 0) {
+#pragma unroll
+            for (int l = 0; l < LN; ++l) reg_w[l] = *reinterpret_cast<const loose16*>(base_w + off_w[l] + at - missing_w);
+        }
+        if (left_a > 0) {
+#pragma unroll
+            for (int l = 0; l < LM; ++l) reg_a[l] = *reinterpret_cast<const loose16*>(base_a + off_a[l] + at - missing_a);
+        }
+#pragma unroll
+        for (int l = 0; l < LN; ++l) reg_w[l] = shifted(reg_w[l], left_w > 0 ? missing_w : 0);
+#pragma unroll
+        for (int l = 0; l < LM; ++l) reg_a[l] = shifted(reg_a[l], left_a > 0 ? missing_a : 0);
     }
     __device__ __forceinline__ void load_scales(int b)
     {
@@ -318,10 +375,12 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
             load_scales(min(group, whole - 1));
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                const int first = min(b * KS + group, whole - 1);
+                before(first);
 #pragma unroll
-                for (int l = 0; l < LN; ++l) bring_w(l, min(b * KS + group, whole - 1), panel_w(b));
+                for (int l = 0; l < LN; ++l) bring_w(l, first, panel_w(b));
 #pragma unroll
-                for (int l = 0; l < LM; ++l) bring_a(l, min(b * KS + group, whole - 1), panel_a(b));
+                for (int l = 0; l < LM; ++l) bring_a(l, first, panel_a(b));
                 put(panel_w(b), panel_a(b));
             }
         }
@@ -380,10 +439,12 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
         if (whole > 0) next_scales();
         int now = 0;                                         // the panel of weights of the group's block i, i % 3
         for (int i = 0; i * KS < whole; ++i) {
+            // past the last whole block the last one again: with a branch the compiler could not count the requests
+            const int next = min((i + 2) * KS + group, whole - 1);
+            before(next);
             // the block has landed (the next one's requests may be on their way), and nobody reads the panel of weights of the block before
             if (DIRECT) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
             else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            // past the last whole block the last one again: with a branch the compiler could not count the requests
             load_scales(min((i + 1) * KS + group, whole - 1));
             __builtin_amdgcn_sched_barrier(0);
             if (KS > 1 && i * KS + group >= whole) {
@@ -392,7 +453,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
                 for (int j = 0; j < FM; ++j) s[j] = 0.f;
             }
             uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(i & 1);
-            block<true>(panel_w(now), to_a, min((i + 2) * KS + group, whole - 1), to_w, to_a);
+            block<true>(panel_w(now), to_a, next, to_w, to_a);
             put(to_w, to_a);
             next_scales();
             now = now == 2 ? 0 : now + 1;
@@ -402,13 +463,8 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
         if (whole < blocks) {
             if (group == 0) {
                 load_scales(whole);
-#pragma unroll 1
-                for (int g = wave; g < (BN + BM) / 8; g += W) {
-                    const bool of_w = g < BN / 8;
-                    const int row = (of_w ? g : g - BN / 8) * 8 + (lane >> 3), at = whole * kBlock + (of_w ? src_w : src_a) * 16;
-                    const uint8_t* from = of_w ? base_w + min(row, last_w) * a.w_stride : base_a + min(row, last_a) * a.a_stride;
-                    *reinterpret_cast<u32x4*>((of_w ? panel_w(0) + g * 1024 : panel_a(0) + (g - BN / 8) * 1024) + lane * 16) = load_piece(from + at, a.k - at);
-                }
+                fetch_end();
+                write_panels(panel_w(0), panel_a(0));
             }
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
             if (group == 0) {
@@ -444,20 +500,22 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int KS = 1> s
                 }
     }
 
-    // The same where K is two whole blocks or more and another tile, at (n1, m1), follows: its first two blocks are requested in this one's last two.
+    // The same where K is two blocks or more, all of them `whole`, and another tile, at (n1, m1), follows: its first two blocks are requested in this one's last two.
     // now, odd: the panels of this tile's first block, then of the next one's.  stores: those issued since the last request, at least.
     __device__ __forceinline__ void multiply_on(int& now, int& odd, bool stores, int n1, int m1)
     {
         clear();
         for (int b = 0; b < whole; ++b) {
+            const int next = b + 2 < whole ? b + 2 : b + 2 - whole;
             if (b == whole - 2) aim_requests(n1, m1);
             if (b == whole - 1) aim_scales(n1, m1);
+            before(next);
             if (b == 0 && stores) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM + FN / 2 * FM) : "memory");
             else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LN + LM) : "memory");
             load_scales(b + 1 < whole ? b + 1 : 0);
             __builtin_amdgcn_sched_barrier(0);
             uint8_t *to_w = panel_w(now == 0 ? 2 : now - 1), *to_a = panel_a(odd);
-            block<true>(panel_w(now), to_a, b + 2 < whole ? b + 2 : b + 2 - whole, to_w, to_a);
+            block<true>(panel_w(now), to_a, next, to_w, to_a);
             next_scales();
             now = now == 2 ? 0 : now + 1;
             odd ^= 1;
@@ -517,7 +575,7 @@ __global__ __launch_bounds__(64 * WN * WM * KS, EU) void matmul_tile_kernel(Matm
     job.store(n * Job::BN, m * Job::BM, a.bias);
 }
 
-// The 256 x 256 tiles, of which a CU holds one, where K is two whole blocks or more: a workgroup for each CU that takes tile after tile of its XCD's, with no break in
+// The 256 x 256 tiles, of which a CU holds one, where K is two blocks or more that are all requested to LDS: a workgroup for each CU that takes tile after tile of its XCD's, with no break in
 // its requests.  Up to 8 tiles that an XCD has left over behind its last whole round of 32 are cut in four for all of its CUs.  (12000 x 11264 x 2048, 8.08 rounds: a
 // workgroup a tile 287 us, this 258; 1500 x 11264 x 2048, 1.03 rounds: 58 and 43.)
 // BIAS: without it a tile's end has nothing that would wait for the requests of the next one.
@@ -588,8 +646,8 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 }
 
 // What a block of K of one tile takes on a GPU that is full of such tiles, in ns (8192 x 8192 x 8192 and, for fp32 and for operands at any address,
-// 4096 x 4096 x 4096).  A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU
-// decide it: 12000 x 11264 x 2048 in us by 256 x 256 in rounds 258, a workgroup a tile 287, 128 x 128 318, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 43, 58, 47, 53, 61;
+// 4096 x 4096 x 4096; in rounds and by 128 x 128, of which one takes over where the other is as fast, 12000 x 2048 x 5632: 140 and 150 us for 2 and 6 rounds of 44 blocks).
+// A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU decide it: 12000 x 11264 x 2048 in us by 256 x 256 in rounds 258, a workgroup a tile 287, 128 x 128 318, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 43, 58, 47, 53, 61;
 // 1500 x 2048 x 5632 33, 59, 25, 28.5, 30; 300 x 11264 x 2048 28, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 12.5, 25.5, 11.8, 8.5, 7.5.
 struct TileCost { int n, m, ns; };
 struct Choice { int tile; bool alone; };                     // alone: a CU has at most one of the tiles
@@ -615,8 +673,8 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
         if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
     }
-    static constexpr TileCost tiles[] = {{256, 256, 1750}, {128, 128, 550}, {128, 64, 340}, {64, 64, 213}};
-    const bool rounds = a.k % kBlock == 0 && a.k >= 2 * kBlock;
+    const bool rounds = a.k % 16 == 0 && a.k > kBlock;
+    const TileCost tiles[] = {{256, 256, rounds ? 1650 : 1750}, {128, 128, 570}, {128, 64, 340}, {64, 64, 213}};
     const Choice c = cheapest(a, tiles, 4, rounds);
     switch (c.tile) {
     case 0: return rounds ? launch_rounds(a, stream) : launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);

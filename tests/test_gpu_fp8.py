@@ -428,7 +428,7 @@ def test_wrong_tensors_are_refused():
 
 
 # 256 x 256 tiles, in rounds where K is a multiple of 128 from 256 on: a last round cut in parts or not, ragged edges, K of 1, 2, 3 and more blocks
-@pytest.mark.parametrize("rows,n,k", [(4096, 4096, 100), (4096, 4096, 128), (4100, 4090, 136), (4096, 4096, 400), (4096, 4096, 256), (4100, 4090, 384), (4097, 4352, 256), (5000, 6200, 512), (2050, 8200, 640), (8200, 8200, 256)])
+@pytest.mark.parametrize("rows,n,k", [(4096, 4096, 100), (4096, 4096, 128), (4100, 4090, 136), (4096, 4096, 144), (4096, 4096, 392), (4096, 4096, 400), (8200, 4400, 272), (4096, 4096, 256), (4100, 4090, 384), (4097, 4352, 256), (5000, 6200, 512), (2050, 8200, 640), (8200, 8200, 256)])
 def test_product_of_many_tiles(rows, n, k):
     g = torch.Generator().manual_seed(rows + n + k)
     whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
@@ -465,3 +465,17 @@ def test_product_of_few_tiles_with_k_in_two_groups(rows, n, k, dtype):
     bad.view(torch.uint8)[5, k - 1] = 0x7f
     got = pa.matmul_fp8(laid_out(bad, aligned), sa, laid_out(w, aligned), sw, dtype=TORCH[dtype])
     assert bool(torch.isnan(got[5]).all()) and int(torch.isnan(got).sum()) == n and torch.equal(got[6:], want[6:].to(TORCH[dtype]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", [(3, 70), (100, 150), (700, 700), (2300, 2100)])
+@pytest.mark.parametrize("k", [1, 7, 15, 16, 17, 31, 48, 113, 127, 129, 143, 160, 255, 272, 383, 399])
+def test_product_of_every_end_of_k(rows, n, k, dtype):
+    """K ends in every place of a block and of a piece; the bytes behind each row are NaN, and so are those before the first and behind the last."""
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+    want = ((a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()).to(TORCH[dtype])
+    for stride, before in ((-(-k // 16) * 16, 16), (k, 0), (k + 5, 3)):
+        assert torch.equal(pa.matmul_fp8(laid_out(a, stride, before), sa, laid_out(w, stride, before), sw, dtype=TORCH[dtype]), want)
