@@ -56,12 +56,15 @@ template <> struct Chunk<float> {
     __device__ void set(int e, float x) { v[e / 4][e % 4] = __float_as_uint(x); }
 };
 
-// Elements 0 .. n - 1 (n < 8) of a chunk; the others stay zero, which no maximum or sum of squares sees.
+// Elements 0 .. n - 1 (0 < n < 8) of a chunk, zeros behind them, which no maximum or sum of squares sees.  All are loaded at once, the last one for those that
+// are not there: behind a branch of its own each would wait for the one before (weights of 517 x 1111 in bf16: 8.6 us, so 6.2; norm of 75 x 5631 6.2 -> 5.2).
 template <typename T> __device__ __forceinline__ void load_tail(Chunk<T>& c, const T* p, int n)
 {
+    T v[7];
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-        if (e < n) c.set(e, p[e]);
+    for (int e = 0; e < 7; ++e) v[e] = p[e < n ? e : n - 1];
+#pragma unroll
+    for (int e = 0; e < 7; ++e) c.set(e, e < n ? v[e] : (T)0);
 }
 
 __device__ __forceinline__ void store8(uint16_t* p, const float (&y)[8])
