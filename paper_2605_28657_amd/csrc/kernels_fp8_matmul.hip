@@ -648,7 +648,9 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 // What a block of K of one tile takes on a GPU that is full of such tiles, in ns (8192 x 8192 x 8192 and, for fp32 and for operands at any address,
 // 4096 x 4096 x 4096; in rounds and by 128 x 128, of which one takes over where the other is as fast, 12000 x 2048 x 5632: 140 and 150 us for 2 and 6 rounds of 44 blocks).
 // A call takes the tile with the smallest sum over its rounds of 256 workgroups, whose ragged last round and whose part-filled GPU decide it: 12000 x 11264 x 2048 in us by 256 x 256 in rounds 258, a workgroup a tile 287, 128 x 128 318, 128 x 64 391, 64 x 64 461; 1500 x 11264 x 2048 43, 58, 47, 53, 61;
-// 1500 x 2048 x 5632 33, 59, 25, 28.5, 30; 300 x 11264 x 2048 28, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 12.5, 25.5, 11.8, 8.5, 7.5.
+// 1500 x 2048 x 5632 33, 59, 25, 28.5, 30; 300 x 11264 x 2048 28, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 12.5, 25.5, 11.8, 8.5, 7.5.  Tiles of 96 rows are for where those of
+// 128 leave CUs without one and those of 64 make another round: 1500 x 2048 x 5632 by 128 x 128 25.3, 128 x 96 22.7, 128 x 64 27.6; 3000 x 2048 x 5632 42, 39, 47;
+// 750 x 2048 x 5632 by 128 x 64 16.5, 64 x 96 15.7, 64 x 64 20; in fp32 42, 38.9, 47; 75, 69, 76; 27.7, 25, 29.
 struct TileCost { int n, m, ns; };
 struct Choice { int tile; bool alone; };                     // alone: a CU has at most one of the tiles
 
@@ -674,12 +676,14 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
         return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
     }
     const bool rounds = a.k % 16 == 0 && a.k > kBlock;
-    const TileCost tiles[] = {{256, 256, rounds ? 1650 : 1750}, {128, 128, 570}, {128, 64, 340}, {64, 64, 213}};
-    const Choice c = cheapest(a, tiles, 4, rounds);
+    const TileCost tiles[] = {{256, 256, rounds ? 1650 : 1750}, {128, 128, 570}, {128, 96, 455}, {128, 64, 340}, {64, 96, 281}, {64, 64, 213}};
+    const Choice c = cheapest(a, tiles, 6, rounds);
     switch (c.tile) {
     case 0: return rounds ? launch_rounds(a, stream) : launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
     case 1: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
-    case 2: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
+    case 2: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 3, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 3, true, 2>(a, stream);
+    case 3: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 2, true, 2>(a, stream);
+    case 4: return c.alone ? launch_tile<uint16_t, 2, 2, 2, 3, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 2, 3, true, 3>(a, stream);
     default: return c.alone ? launch_tile<uint16_t, 2, 2, 2, 2, true, 4, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 2, 2, true, 4>(a, stream);
     }
 }
@@ -691,11 +695,13 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
         if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
     }
-    static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 64, 570}, {64, 64, 305}};
-    const Choice c = cheapest(a, tiles, 3, false);
+    static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 96, 800}, {128, 64, 570}, {64, 96, 445}, {64, 64, 305}};
+    const Choice c = cheapest(a, tiles, 5, false);
     switch (c.tile) {
     case 0: return c.alone ? launch_tile<float, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
-    case 1: return c.alone ? launch_tile<float, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
+    case 1: return c.alone ? launch_tile<float, 2, 2, 4, 3, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 3, true, 2>(a, stream);
+    case 2: return c.alone ? launch_tile<float, 2, 2, 4, 2, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 2, true, 2>(a, stream);
+    case 3: return c.alone ? launch_tile<float, 2, 2, 2, 3, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 2, 3, true, 3>(a, stream);
     default: return c.alone ? launch_tile<float, 2, 2, 2, 2, true, 3, 2>(a, stream) : launch_tile<float, 2, 2, 2, 2, true, 3>(a, stream);
     }
 }

@@ -479,3 +479,21 @@ def test_product_of_every_end_of_k(rows, n, k, dtype):
     want = ((a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()).to(TORCH[dtype])
     for stride, before in ((-(-k // 16) * 16, 16), (k, 0), (k + 5, 3)):
         assert torch.equal(pa.matmul_fp8(laid_out(a, stride, before), sa, laid_out(w, stride, before), sw, dtype=TORCH[dtype]), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", [(1460, 2000), (2950, 2040), (740, 2010), (5900, 705), (1000, 3800)])
+@pytest.mark.parametrize("k", [128, 272, 1111, 1152])
+def test_product_of_counts_of_rows_between_those_of_the_square_tiles(rows, n, k, dtype):
+    """Tiles of 96 rows, one a compute unit and more, with rows and columns that end inside a tile; bias and the latent layout with them."""
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+    bias = torch.randint(-9, 10, (n,), generator=g).float().to(DEV)
+    want = ((a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t() + bias).to(TORCH[dtype])
+    aligned = -(-k // 16) * 16
+    la, lw = laid_out(a, aligned), laid_out(w, aligned)
+    assert torch.equal(pa.matmul_fp8(la, sa, lw, sw, bias=bias, dtype=TORCH[dtype]), want)
+    latent = pa.matmul_fp8(la, sa, lw, sw, bias=bias, dtype=TORCH[dtype], n_frames=rows // 5)
+    assert torch.equal(latent, want.view(5, rows // 5, n).transpose(1, 2))
