@@ -706,14 +706,18 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
     }
 }
 
-// Few outputs go without LDS: 16 x 16 outputs a workgroup for one tile of rows (1 x 8192 x 8192 in us 14, 64 x 64 tiles 21; 8 x 11264 x 2048 7.4 and 7.9) or where
-// the GPU is not full of such workgroups (32 x 2048 x 2048 4.6 and 7.2), 32 x 16 up to 320 of them (64 x 2048 x 2048 5.4 and 7.2; 64 x 11264 x 2048, which
-// has 1408, 20 and 8.8).  So do operands whose rows lie too far apart for 32-bit offsets in a tile.
+// Few outputs go without LDS: one tile of rows (8 x 11264 x 2048 in us 7.6, 64 x 64 tiles 7.9; 1 x 8192 x 8192 14 and 21), or where the GPU is not full of such workgroups,
+// of 16 x 16 outputs (32 x 2048 x 2048 4.6 and 7.2) or up to 320 of 32 x 16 (64 x 2048 x 2048 5.4 and 7.2; 64 x 11264 x 2048, which has 1408, 20 and 8.8).  So do
+// operands whose rows lie too far apart for 32-bit offsets in a tile.
+// One tile of rows by 16 weight rows with 8 waves up to a workgroup for each CU (16 x 4096 x 4096 7.1, by 32 with 4 waves 8.3), by 32 with 4 behind that, which reads `a` half
+// as often (16 x 5632 x 2048 6.6 and 5.6, 16 x 16384 x 2048 11.8 and 8.6, 1 x 32000 x 2048 17.4 and 12.5; at worst 1 x 11264 x 8320 18 and 21), but not
+// where the weights' rows lie a multiple of 8 KB apart, and 32 of them on as few channels of memory (1 x 8192 x 8192 14 and 19.7, 1 x 16384 x 8192 29 and 35).
 template <typename O> static hipError_t launch(const MatmulFp8& a, hipStream_t stream)
 {
     const bool aligned = (((uintptr_t)a.a | (uintptr_t)a.w | (uintptr_t)a.a_stride | (uintptr_t)a.w_stride) & 15) == 0;
     const bool near = a.a_stride < (1 << 22) && a.w_stride < (1 << 22);
     const long long rows16 = (a.rows + 15) / 16, n16 = (a.n + 15) / 16, n32 = (a.n + 31) / 32;
+    if (rows16 == 1 && n16 > 256 && a.w_stride % 8192 != 0) return launch_direct<O, 2, 1, 4, 2>(a, stream);
     if (rows16 == 1 || rows16 * n16 <= 256) return launch_direct<O, 1, 1, 8, 2>(a, stream);
     if (rows16 * n32 <= 320 || !near) return launch_direct<O, 2, 1, 8, 2>(a, stream);
     return launch_tiles(a, O(), aligned, stream);

@@ -497,3 +497,21 @@ def test_product_of_counts_of_rows_between_those_of_the_square_tiles(rows, n, k,
     assert torch.equal(pa.matmul_fp8(la, sa, lw, sw, bias=bias, dtype=TORCH[dtype]), want)
     latent = pa.matmul_fp8(la, sa, lw, sw, bias=bias, dtype=TORCH[dtype], n_frames=rows // 5)
     assert torch.equal(latent, want.view(5, rows // 5, n).transpose(1, 2))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,k", [(1, 4097, 128), (1, 4113, 1111), (3, 4200, 15), (9, 5000, 300), (16, 8200, 2064), (2, 4500, 8192), (15, 4103, 4500), (16, 4096, 1200)])
+def test_product_of_few_rows_with_many_weights(rows, n, k, dtype):
+    """Up to a tile of rows with more weight rows than one workgroup a compute unit takes; the bytes behind each row are NaN, and so are those before the first and behind the last."""
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+    bias = torch.randint(-9, 10, (n,), generator=g).float().to(DEV)
+    want = ((a.double() * at_rows(sa, k)) @ (w.double() * at_weights(sw, n, k)).t() + bias).float()
+    assert float(want.abs().max()) < 2 ** 14                         # whole numbers of quarters: fp32 has every sum exactly
+    for stride, before in ((-(-k // 16) * 16, 16), (k, 0), (k + 5, 3)):
+        got = pa.matmul_fp8(laid_out(a, stride, before), sa, laid_out(w, stride, before), sw, bias=bias, dtype=TORCH[dtype])
+        assert torch.equal(got, want.to(TORCH[dtype]))
+    latent = pa.matmul_fp8(a, sa, w, sw, bias=bias, dtype=TORCH[dtype], n_frames=1)
+    assert torch.equal(latent, want.to(TORCH[dtype]).view(rows, n, 1))
