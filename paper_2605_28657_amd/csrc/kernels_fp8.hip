@@ -307,7 +307,8 @@ hipError_t launch_rms_norm_fp8(const RowsFp8& a, const NormFp8& n, bool bf16, hi
 }
 
 // ---------------------------------------------------------------------------------- weights
-// A workgroup takes a 128 x 128 block: a row of it in 16 lanes, 8 rows a thread, held in registers between the maximum and the write.
+// A workgroup takes a 128 x 128 block: a row of it in 16 lanes, 8 rows a thread, held in registers between the maximum and the write.  Bound by the bytes
+// (11264 x 2048 in bf16, 69 MB, 11.8 us: 5900 GB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_weights_kernel(const T* __restrict__ w, long long w_stride, int n, int k, uint8_t* __restrict__ q,
                                                                long long q_stride, float* __restrict__ scale)

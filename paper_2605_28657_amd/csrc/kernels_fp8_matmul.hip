@@ -143,7 +143,8 @@ template <typename O> __device__ __forceinline__ void store_row(const MatmulFp8&
 
 // ---------------------------------------------------------------------------------- operands straight from memory
 // A workgroup of W waves takes 16 FN weight rows by 16 FM rows; each wave sums every W-th block of K, from operands that it loads into
-// registers itself, and the waves' sums are added in their order through LDS.  Reads any alignment and any K.
+// registers itself, and the waves' sums are added in their order through LDS.  Reads any alignment and any K.  It is bound by the bytes of the weights where they are many (1 x 32000 x 2048
+// 12.5 us, 5240 GB/s) and by the latency of a launch and of two or three dependent loads where not (1 x 2048 x 2048 3.8 us, an empty launch 2.1).
 template <typename O, int FN, int FM, int W, int U>
 __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 {
