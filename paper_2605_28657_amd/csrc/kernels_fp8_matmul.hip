@@ -653,9 +653,11 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 // 128 leave CUs without one and those of 64 make another round: 1500 x 2048 x 5632 by 128 x 128 25.3, 128 x 96 22.7, 128 x 64 27.6; 3000 x 2048 x 5632 42, 39, 47;
 // 750 x 2048 x 5632 by 128 x 64 16.5, 64 x 96 15.7, 64 x 64 20; in fp32 42, 38.9, 47; 75, 69, 76; 27.7, 25, 29.
 struct TileCost { int n, m, ns; };
-struct Choice { int tile; bool alone; };                     // alone: a CU has at most one of the tiles
+// alone: a CU has at most one of the tiles, and K is long enough for two groups to gain more than their join takes: from 9 blocks on, with the longer products of an fp32 output from 6
+// (500 x 640 x 640 by one 4.1 us, by two 4.6, in fp32 5.5 and 5.8; 300 x 2560 x 1024 5.0 and 5.2, in fp32 7.1 and 6.7)
+struct Choice { int tile; bool alone; };
 
-static Choice cheapest(const MatmulFp8& a, const TileCost* tiles, int count, bool first_in_rounds)
+static Choice cheapest(const MatmulFp8& a, const TileCost* tiles, int count, bool first_in_rounds, int join_blocks)
 {
     Choice best = {0, false};
     long long least = 0;
@@ -664,7 +666,7 @@ static Choice cheapest(const MatmulFp8& a, const TileCost* tiles, int count, boo
         long long cost = (all + 255) / 256 * tiles[i].ns;
         // matmul_rounds_kernel: a last round of up to 8 tiles an XCD takes two fifths of a round
         if (const long long left = (all + 7) / 8 % 32; i == 0 && first_in_rounds && left > 0 && left <= 8) cost -= tiles[i].ns * 3 / 5;
-        if (i == 0 || cost < least) { best = {i, all <= 256}; least = cost; }
+        if (i == 0 || cost < least) { best = {i, all <= 256 && a.k > join_blocks * kBlock}; least = cost; }
     }
     return best;
 }
@@ -673,12 +675,12 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 640}};
-        if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false, 0).tile == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
     }
     const bool rounds = a.k % 16 == 0 && a.k > kBlock;
     const TileCost tiles[] = {{256, 256, rounds ? 1650 : 1750}, {128, 128, 570}, {128, 96, 455}, {128, 64, 340}, {64, 96, 281}, {64, 64, 213}};
-    const Choice c = cheapest(a, tiles, 6, rounds);
+    const Choice c = cheapest(a, tiles, 6, rounds, 8);
     switch (c.tile) {
     case 0: return rounds ? launch_rounds(a, stream) : launch_tile<uint16_t, 2, 4, 8, 4, true, 2>(a, stream);
     case 1: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 4, true, 2>(a, stream);
@@ -693,11 +695,11 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
 {
     if (!aligned) {
         static constexpr TileCost tiles[] = {{128, 128, 1220}, {128, 64, 780}};
-        if (cheapest(a, tiles, 2, false).tile == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
+        if (cheapest(a, tiles, 2, false, 0).tile == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
         return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
     }
     static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 96, 800}, {128, 64, 570}, {64, 96, 445}, {64, 64, 305}};
-    const Choice c = cheapest(a, tiles, 5, false);
+    const Choice c = cheapest(a, tiles, 5, false, 5);
     switch (c.tile) {
     case 0: return c.alone ? launch_tile<float, 2, 2, 4, 4, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 4, true, 2>(a, stream);
     case 1: return c.alone ? launch_tile<float, 2, 2, 4, 3, true, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 3, true, 2>(a, stream);
@@ -708,7 +710,7 @@ static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStrea
 }
 
 // Few outputs go without LDS: one tile of rows (8 x 11264 x 2048 in us 7.6, 64 x 64 tiles 7.9; 1 x 8192 x 8192 14 and 21), or where the GPU is not full of such workgroups,
-// of 16 x 16 outputs (32 x 2048 x 2048 4.6 and 7.2) or up to 320 of 32 x 16 (64 x 2048 x 2048 5.4 and 7.2; 64 x 11264 x 2048, which has 1408, 20 and 8.8).  So do
+// of 16 x 16 outputs (32 x 2048 x 2048 4.6 and 7.2) or of 32 x 16 (64 x 2048 x 2048 5.4 and 7.2; 150 x 1024 x 2048, which has 320, 8.1 and 6.7, in fp32 8.2 and 9.1).  So do
 // operands whose rows lie too far apart for 32-bit offsets in a tile.
 // One tile of rows by 16 weight rows with 8 waves up to a workgroup for each CU (16 x 4096 x 4096 7.1, by 32 with 4 waves 8.3), by 32 with 4 behind that, which reads `a` half
 // as often (16 x 5632 x 2048 6.6 and 5.6, 16 x 16384 x 2048 11.8 and 8.6, 1 x 32000 x 2048 17.4 and 12.5; at worst 1 x 11264 x 8320 18 and 21), but not
@@ -720,7 +722,7 @@ template <typename O> static hipError_t launch(const MatmulFp8& a, hipStream_t s
     const long long rows16 = (a.rows + 15) / 16, n16 = (a.n + 15) / 16, n32 = (a.n + 31) / 32;
     if (rows16 == 1 && n16 > 256 && a.w_stride % 8192 != 0) return launch_direct<O, 2, 1, 4, 2>(a, stream);
     if (rows16 == 1 || rows16 * n16 <= 256) return launch_direct<O, 1, 1, 8, 2>(a, stream);
-    if (rows16 * n32 <= 320 || !near) return launch_direct<O, 2, 1, 8, 2>(a, stream);
+    if (rows16 * n32 <= (sizeof(O) == 2 ? 256 : 320) || !near) return launch_direct<O, 2, 1, 8, 2>(a, stream);
     return launch_tiles(a, O(), aligned, stream);
 }
 
