@@ -76,7 +76,7 @@ __device__ __forceinline__ u32x4 shifted(u32x4 v, int missing)
 }
 
 // A piece of 16 values at p, of which the first `left` belong to a row of k values; zeros for the others, which are not read.  The piece that a row of 16 values or
-// more ends in is the row's last 16 bytes, shifted: one load.  (Byte by byte, each behind a branch of its own, it takes 15 one after another: 600 x 2048 x 2047
+// more ends in is the row's last 16 bytes, shifted: one load.  (Byte by byte, each behind a branch of its own, it takes 15 one after another: 600 x 2048 x 2047 by 128 x 64 tiles
 // 27.5 us, this 20.7.)
 __device__ __forceinline__ u32x4 load_piece(const uint8_t* p, int left, int k)
 {
@@ -652,6 +652,7 @@ template <typename O, int FN, int FM, int W, int U> static hipError_t launch_dir
 // 1500 x 2048 x 5632 33, 59, 25, 28.5, 30; 300 x 11264 x 2048 28, 28, 17.6, 13.8, 16.7; 64 x 11264 x 2048 12.5, 25.5, 11.8, 8.5, 7.5.  Tiles of 96 rows are for where those of
 // 128 leave CUs without one and those of 64 make another round: 1500 x 2048 x 5632 by 128 x 128 25.3, 128 x 96 22.7, 128 x 64 27.6; 3000 x 2048 x 5632 42, 39, 47;
 // 750 x 2048 x 5632 by 128 x 64 16.5, 64 x 96 15.7, 64 x 64 20; in fp32 42, 38.9, 47; 75, 69, 76; 27.7, 25, 29.
+// Operands at any address (rows 3 bytes off): 1500 x 2048 x 5632 by 128 x 128 in two groups 50, in one 56, 128 x 64 57, 64 x 64 60; 300 x 2048 x 5632 50, 57, 39 (in two), 30 (in two).
 struct TileCost { int n, m, ns; };
 // alone: a CU has at most one of the tiles, and K is long enough for two groups to gain more than their join takes: from 9 blocks on, with the longer products of an fp32 output from 6
 // (500 x 640 x 640 by one 4.1 us, by two 4.6, in fp32 5.5 and 5.8; 300 x 2560 x 1024 5.0 and 5.2, in fp32 7.1 and 6.7)
@@ -674,9 +675,13 @@ static Choice cheapest(const MatmulFp8& a, const TileCost* tiles, int count, boo
 static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipStream_t stream)
 {
     if (!aligned) {
-        static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 640}};
-        if (cheapest(a, tiles, 2, false, 0).tile == 0) return launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
-        return launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
+        static constexpr TileCost tiles[] = {{128, 128, 890}, {128, 64, 630}, {64, 64, 417}};
+        const Choice c = cheapest(a, tiles, 3, false, 8);
+        switch (c.tile) {
+        case 0: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 4, false, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 4, false, 2>(a, stream);
+        case 1: return c.alone ? launch_tile<uint16_t, 2, 2, 4, 2, false, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 4, 2, false, 2>(a, stream);
+        default: return c.alone ? launch_tile<uint16_t, 2, 2, 2, 2, false, 2, 2>(a, stream) : launch_tile<uint16_t, 2, 2, 2, 2, false, 3>(a, stream);
+        }
     }
     const bool rounds = a.k % 16 == 0 && a.k > kBlock;
     const TileCost tiles[] = {{256, 256, rounds ? 1650 : 1750}, {128, 128, 570}, {128, 96, 455}, {128, 64, 340}, {64, 96, 281}, {64, 64, 213}};
@@ -694,9 +699,13 @@ static hipError_t launch_tiles(const MatmulFp8& a, uint16_t, bool aligned, hipSt
 static hipError_t launch_tiles(const MatmulFp8& a, float, bool aligned, hipStream_t stream)
 {
     if (!aligned) {
-        static constexpr TileCost tiles[] = {{128, 128, 1220}, {128, 64, 780}};
-        if (cheapest(a, tiles, 2, false, 0).tile == 0) return launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
-        return launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
+        static constexpr TileCost tiles[] = {{128, 128, 1190}, {128, 64, 760}, {64, 64, 439}};
+        const Choice c = cheapest(a, tiles, 3, false, 5);
+        switch (c.tile) {
+        case 0: return c.alone ? launch_tile<float, 2, 2, 4, 4, false, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 4, false, 2>(a, stream);
+        case 1: return c.alone ? launch_tile<float, 2, 2, 4, 2, false, 2, 2>(a, stream) : launch_tile<float, 2, 2, 4, 2, false, 2>(a, stream);
+        default: return c.alone ? launch_tile<float, 2, 2, 2, 2, false, 2, 2>(a, stream) : launch_tile<float, 2, 2, 2, 2, false, 3>(a, stream);
+        }
     }
     static constexpr TileCost tiles[] = {{128, 128, 970}, {128, 96, 800}, {128, 64, 570}, {64, 96, 445}, {64, 64, 305}};
     const Choice c = cheapest(a, tiles, 5, false, 5);

@@ -515,3 +515,17 @@ def test_product_of_few_rows_with_many_weights(rows, n, k, dtype):
         assert torch.equal(got, want.to(TORCH[dtype]))
     latent = pa.matmul_fp8(a, sa, w, sw, bias=bias, dtype=TORCH[dtype], n_frames=1)
     assert torch.equal(latent, want.to(TORCH[dtype]).view(rows, n, 1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", [(420, 1104), (700, 1030), (1800, 1100), (1500, 2048), (2300, 2100)])
+@pytest.mark.parametrize("k", [640, 700, 1152, 1279, 1291])
+def test_product_of_operands_at_any_address(rows, n, k, dtype):
+    """Every tile for operands that are not 16 bytes apart, K in one and in two groups of waves; what lies around the rows is NaN."""
+    g = torch.Generator().manual_seed(rows + n + k)
+    whole = lambda *shape: torch.randint(-4, 5, shape, generator=g).float().to(E4M3).to(DEV)      # noqa: E731
+    powers = lambda *shape: torch.exp2(torch.randint(-1, 2, shape, generator=g).float()).to(DEV)  # noqa: E731
+    a, w, sa, sw = whole(rows, k), whole(n, k), powers(blocks(k), rows), powers(blocks(n), blocks(k))
+    want = ((a.float() * at_rows(sa, k)) @ (w.float() * at_weights(sw, n, k)).t()).to(TORCH[dtype])
+    for stride, before in ((k | 1, 0), (k + 5, 3)):
+        assert torch.equal(pa.matmul_fp8(laid_out(a, stride, before), sa, laid_out(w, stride, before), sw, dtype=TORCH[dtype]), want)
