@@ -9,6 +9,7 @@ from .binding import (DemonVAE, DemonVAEEncoder, DemonError, demon_vae_create_en
                       demon_vae_set_timing, demon_vae_get_timing, demon_vae_latent_similarity, demon_vae_crossfade,
                       latent_similarity, crossfade,
                       demon_vae_quantize_fp8, demon_vae_rms_norm_fp8, demon_vae_quantize_weights_fp8, demon_vae_matmul_fp8,
+                      demon_vae_matmul_fp8_fp32_sums,
                       quantize_fp8, rms_norm_fp8, quantize_weights_fp8, matmul_fp8,
                       DEMON_OK, DEMON_ERR_INVALID_ARG, DEMON_ERR_UNSUPPORTED, DEMON_ERR_WORKSPACE, DEMON_ERR_HIP,
                       DEMON_F32, DEMON_BF16, DEMON_VAE_FLAG_NO_FUSED, DEMON_VAE_FLAG_ONE_STREAM, DEMON_VAE_FLAG_NO_WIDE_TILE, DEMON_VAE_FLAG_NO_HEAD_FUSION)

@@ -90,6 +90,7 @@ def load_library() -> ctypes.CDLL:
                                                    ctypes.c_void_p, ctypes.c_void_p]
     lib.demon_vae_matmul_fp8.argtypes = [ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, LL, ctypes.c_void_p, ctypes.c_void_p,
                                          ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, LL, ctypes.c_void_p]
+    lib.demon_vae_matmul_fp8_fp32_sums.argtypes = lib.demon_vae_matmul_fp8.argtypes
     lib.demon_vae_debug_tap.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t]
     lib.demon_vae_debug_callers_grid.argtypes = [ctypes.c_void_p, ctypes.c_int]
     lib.demon_vae_debug_last_grid.argtypes = [ctypes.c_void_p, P(ctypes.c_int), P(ctypes.c_longlong), P(ctypes.c_int)]
@@ -321,6 +322,13 @@ def demon_vae_matmul_fp8(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride
                                                n_frames, out_dtype, d_out, out_stride, stream))
 
 
+def demon_vae_matmul_fp8_fp32_sums(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride: int, d_w: int, w_stride: int, d_w_scale: int,
+                                   d_bias: int, rows: int, n: int, k: int, n_frames: int, out_dtype: int, d_out: int, out_stride: int,
+                                   stream: int = 0):
+    _check(load_library().demon_vae_matmul_fp8_fp32_sums(d_a, a_stride, d_a_scale, a_scale_stride, d_w, w_stride, d_w_scale, d_bias, rows, n, k,
+                                                         n_frames, out_dtype, d_out, out_stride, stream))
+
+
 # These operators are called once or more in every layer on a few rows: a call's host time is part of what they are.
 def _launch(fn, device, *args):
     """fn(*args, stream) on the current stream of `device`, with that device current."""
@@ -444,10 +452,14 @@ def quantize_weights_fp8(w, out=None):
     return q, scale
 
 
-def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0, out=None):
+def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0, out=None, fp32_sums: bool = False):
     """a w^T (+ bias) of rows (q, scale) of quantize_fp8 or rms_norm_fp8, a [rows, k], and weights (q, scale) of quantize_weights_fp8,
     w [n, k]: [rows, n] in `dtype` (bf16, the default, or fp32), or with n_frames > 0 the latent [rows / n_frames, n, n_frames] of rows
-    clip * n_frames + frame.  bias: fp32 [n].  `out`: a tensor to write into (its dtype is taken)."""
+    clip * n_frames + frame.  bias: fp32 [n].  `out`: a tensor to write into (its dtype is taken).
+
+    An fp32 output has fp32 sums.  A bf16 output has those of the 8-bit matrix instructions, which keep 13 bits behind the largest of every 8 products: off by up
+    to 2^-10.2 of the sum of the products' magnitudes, less than a quarter of the output's rounding unless products cancel.  With `fp32_sums` it is the fp32
+    output rounded, at half the rate."""
     import torch
     device = a.device
     rows, k = a.shape
@@ -464,7 +476,8 @@ def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0,
     else:
         assert out.shape == shape and out.device == device and (dtype is None or dtype is out.dtype) and (n_frames == 0 or out.is_contiguous())
         os_ = 0 if n_frames else _apart(_matrix(out, out.dtype, device), n, rows)
-    _launch(load_library().demon_vae_matmul_fp8, device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
+    lib = load_library()
+    _launch(lib.demon_vae_matmul_fp8_fp32_sums if fp32_sums else lib.demon_vae_matmul_fp8, device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
             w_scale.data_ptr(), 0 if bias is None else bias.data_ptr(), rows, n, k, n_frames, _demon_dtype(out.dtype), out.data_ptr(), os_)
     return out
 

@@ -24,6 +24,20 @@ demon_status check_rows(int rows, int channels, demon_dtype dtype, const void* q
     return DEMON_OK;
 }
 
+demon_status matmul(const MatmulFp8& a, demon_dtype out_dtype, bool fp32_sums, void* stream)
+{
+    clear_error();
+    if (!a.a || !a.a_scale || !a.w || !a.w_scale || !a.out) return fail(DEMON_ERR_INVALID_ARG, "NULL argument");
+    if (a.rows < 1 || a.n < 1 || a.k < 1) return fail(DEMON_ERR_INVALID_ARG, "rows, n and k must be >= 1");
+    if (out_dtype != DEMON_F32 && out_dtype != DEMON_BF16) return fail(DEMON_ERR_INVALID_ARG, "unknown dtype");
+    if (a.a_stride < 0 || a.w_stride < 0) return fail(DEMON_ERR_INVALID_ARG, "negative row stride");
+    if (a.a_scale_stride < a.rows) return fail(DEMON_ERR_INVALID_ARG, "scales of blocks overlap");
+    if (a.n_frames < 0 || (a.n_frames > 0 && a.rows % a.n_frames != 0)) return fail(DEMON_ERR_INVALID_ARG, "rows must be a multiple of n_frames");
+    if (a.n_frames == 0 && a.out_stride < a.n) return fail(DEMON_ERR_INVALID_ARG, "output rows overlap");
+    if (a.rows > (1 << 24) || a.n > (1 << 24) || a.k > (1 << 24)) return fail(DEMON_ERR_UNSUPPORTED, "more than 16777216 rows, columns or values of K");
+    return launched(launch_matmul_fp8(a, out_dtype == DEMON_BF16, fp32_sums, (hipStream_t)stream), "matrix product");
+}
+
 }  // namespace
 
 extern "C" {
@@ -76,18 +90,18 @@ demon_status demon_vae_matmul_fp8(const void* d_a, long long a_stride, const flo
                                   const void* d_w, long long w_stride, const float* d_w_scale, const float* d_bias, int rows, int n, int k,
                                   int n_frames, demon_dtype out_dtype, void* d_out, long long out_stride, void* stream)
 {
-    clear_error();
-    if (!d_a || !d_a_scale || !d_w || !d_w_scale || !d_out) return fail(DEMON_ERR_INVALID_ARG, "NULL argument");
-    if (rows < 1 || n < 1 || k < 1) return fail(DEMON_ERR_INVALID_ARG, "rows, n and k must be >= 1");
-    if (out_dtype != DEMON_F32 && out_dtype != DEMON_BF16) return fail(DEMON_ERR_INVALID_ARG, "unknown dtype");
-    if (a_stride < 0 || w_stride < 0) return fail(DEMON_ERR_INVALID_ARG, "negative row stride");
-    if (a_scale_stride < rows) return fail(DEMON_ERR_INVALID_ARG, "scales of blocks overlap");
-    if (n_frames < 0 || (n_frames > 0 && rows % n_frames != 0)) return fail(DEMON_ERR_INVALID_ARG, "rows must be a multiple of n_frames");
-    if (n_frames == 0 && out_stride < n) return fail(DEMON_ERR_INVALID_ARG, "output rows overlap");
-    if (rows > (1 << 24) || n > (1 << 24) || k > (1 << 24)) return fail(DEMON_ERR_UNSUPPORTED, "more than 16777216 rows, columns or values of K");
     const MatmulFp8 a = {(const uint8_t*)d_a, a_stride, d_a_scale, a_scale_stride, (const uint8_t*)d_w, w_stride, d_w_scale, d_bias,
                          d_out, out_stride, rows, n, k, n_frames};
-    return launched(launch_matmul_fp8(a, out_dtype == DEMON_BF16, (hipStream_t)stream), "matrix product");
+    return matmul(a, out_dtype, false, stream);
+}
+
+demon_status demon_vae_matmul_fp8_fp32_sums(const void* d_a, long long a_stride, const float* d_a_scale, long long a_scale_stride,
+                                            const void* d_w, long long w_stride, const float* d_w_scale, const float* d_bias, int rows, int n, int k,
+                                            int n_frames, demon_dtype out_dtype, void* d_out, long long out_stride, void* stream)
+{
+    const MatmulFp8 a = {(const uint8_t*)d_a, a_stride, d_a_scale, a_scale_stride, (const uint8_t*)d_w, w_stride, d_w_scale, d_bias,
+                         d_out, out_stride, rows, n, k, n_frames};
+    return matmul(a, out_dtype, true, stream);
 }
 
 }  // extern "C"
