@@ -298,26 +298,40 @@ def crossfade(prev_tail, next_head, out=None):
     return out
 
 
+_LARGEST_SIZE = 0x7fffffff
+
+
+def _check_sizes(*sizes: int):
+    """The C entries take sizes of 32 bits, and ctypes would pass a larger one's low 32 bits as if that were all."""
+    for size in sizes:
+        if not -_LARGEST_SIZE <= size <= _LARGEST_SIZE:
+            raise DemonError(DEMON_ERR_UNSUPPORTED, f"a size of {size}")
+
+
 def demon_vae_quantize_fp8(d_x: int, x_stride: int, rows: int, channels: int, gated: int, dtype: int, d_q: int, q_stride: int,
                            d_scale: int, scale_stride: int, stream: int = 0):
+    _check_sizes(rows, channels)
     _check(load_library().demon_vae_quantize_fp8(d_x, x_stride, rows, channels, gated, dtype, d_q, q_stride, d_scale, scale_stride, stream))
 
 
 def demon_vae_rms_norm_fp8(d_x: int, x_stride: int, d_residual: int, residual_stride: int, d_weight: int, rows: int, channels: int,
                            eps: float, dtype: int, d_sum: int, sum_stride: int, d_q: int, q_stride: int, d_scale: int,
                            scale_stride: int, stream: int = 0):
+    _check_sizes(rows, channels)
     _check(load_library().demon_vae_rms_norm_fp8(d_x, x_stride, d_residual, residual_stride, d_weight, rows, channels, eps, dtype,
                                                  d_sum, sum_stride, d_q, q_stride, d_scale, scale_stride, stream))
 
 
 def demon_vae_quantize_weights_fp8(d_w: int, w_stride: int, n: int, k: int, dtype: int, d_q: int, q_stride: int, d_scale: int,
                                    stream: int = 0):
+    _check_sizes(n, k)
     _check(load_library().demon_vae_quantize_weights_fp8(d_w, w_stride, n, k, dtype, d_q, q_stride, d_scale, stream))
 
 
 def demon_vae_matmul_fp8(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride: int, d_w: int, w_stride: int, d_w_scale: int,
                          d_bias: int, rows: int, n: int, k: int, n_frames: int, out_dtype: int, d_out: int, out_stride: int,
                          stream: int = 0):
+    _check_sizes(rows, n, k, n_frames)
     _check(load_library().demon_vae_matmul_fp8(d_a, a_stride, d_a_scale, a_scale_stride, d_w, w_stride, d_w_scale, d_bias, rows, n, k,
                                                n_frames, out_dtype, d_out, out_stride, stream))
 
@@ -325,6 +339,7 @@ def demon_vae_matmul_fp8(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride
 def demon_vae_matmul_fp8_fp32_sums(d_a: int, a_stride: int, d_a_scale: int, a_scale_stride: int, d_w: int, w_stride: int, d_w_scale: int,
                                    d_bias: int, rows: int, n: int, k: int, n_frames: int, out_dtype: int, d_out: int, out_stride: int,
                                    stream: int = 0):
+    _check_sizes(rows, n, k, n_frames)
     _check(load_library().demon_vae_matmul_fp8_fp32_sums(d_a, a_stride, d_a_scale, a_scale_stride, d_w, w_stride, d_w_scale, d_bias, rows, n, k,
                                                          n_frames, out_dtype, d_out, out_stride, stream))
 
@@ -398,6 +413,8 @@ def quantize_fp8(x, gated: bool = False, out=None):
     if gated:
         assert channels % 2 == 0
         channels //= 2
+    if rows | channels > _LARGEST_SIZE:
+        _check_sizes(rows, channels)
     q, qs, scale, ss = _fp8_rows(x, rows, channels, out)
     _launch(load_library().demon_vae_quantize_fp8, device, x.data_ptr(), xs, rows, channels, int(gated), dtype, q.data_ptr(), qs, scale.data_ptr(), ss)
     return q, scale
@@ -412,6 +429,8 @@ def rms_norm_fp8(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=
     dtype = _demon_dtype(xt)
     xs = _matrix(x, xt, device)
     rows, channels = shape = x.shape
+    if rows | channels > _LARGEST_SIZE:
+        _check_sizes(rows, channels)
     assert weight.dtype is torch.float32 and weight.shape == (channels,) and weight.is_contiguous() and weight.device == device
     xp, rp, rs, hp, hs = x.data_ptr(), 0, 0, 0, 0
     if residual is not None:
@@ -440,6 +459,8 @@ def quantize_weights_fp8(w, out=None):
     device = w.device
     ws = _matrix(w, w.dtype, device)
     n, k = w.shape
+    if n | k > _LARGEST_SIZE:
+        _check_sizes(n, k)
     blocks = (-(-n // 128), -(-k // 128))
     if out is None:
         q, scale = _new_fp8(w, n, k), w.new_empty(blocks, dtype=torch.float32)
@@ -464,6 +485,8 @@ def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0,
     device = a.device
     rows, k = a.shape
     n = w.shape[0]
+    if rows | n | k | n_frames > _LARGEST_SIZE:
+        _check_sizes(rows, n, k, n_frames)
     blocks = -(-k // 128)
     as_, ws = _matrix(a, torch.float8_e4m3fn, device), _matrix(w, torch.float8_e4m3fn, device)
     ss, _ = _matrix(a_scale, torch.float32, device), _matrix(w_scale, torch.float32, device)
