@@ -268,8 +268,10 @@ def latent_similarity(curr, prev, threshold: float = 1e-3):
     import torch
     if curr.dim() == 2:
         curr, prev = curr[None], prev[None]
-    assert curr.is_cuda and prev.is_cuda and curr.shape == prev.shape and curr.dtype == prev.dtype
-    assert curr.is_contiguous() and prev.is_contiguous()
+    if not (curr.is_cuda and prev.is_cuda and curr.shape == prev.shape and curr.dtype == prev.dtype):
+        raise AssertionError("latents of one shape and type on the GPU")
+    if not (curr.is_contiguous() and prev.is_contiguous()):
+        raise AssertionError("contiguous latents")
     dtype = {torch.bfloat16: DEMON_BF16, torch.float32: DEMON_F32}[curr.dtype]
     n = curr.shape[0]
     mse = torch.empty(n, dtype=torch.float32, device=curr.device)
@@ -286,13 +288,15 @@ def crossfade(prev_tail, next_head, out=None):
 
     def planes(t):
         t2 = t.reshape(-1, t.shape[-1]) if t.is_contiguous() else t
-        assert t2.dim() == 2 and t2.stride(1) == 1 and t2.dtype == torch.float32 and t2.is_cuda
+        if not (t2.dim() == 2 and t2.stride(1) == 1 and t2.dtype == torch.float32 and t2.is_cuda):
+            raise AssertionError("fp32 planes on the GPU whose samples follow each other")
         return t2
 
     if out is None:
         out = torch.empty(prev_tail.shape, dtype=torch.float32, device=prev_tail.device)
     a, b, o = planes(prev_tail), planes(next_head), planes(out)
-    assert a.shape == b.shape == o.shape
+    if not (a.shape == b.shape == o.shape):
+        raise AssertionError("planes of one shape")
     demon_vae_crossfade(a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0), o.data_ptr(), o.stride(0),
                         a.shape[0], a.shape[1], torch.cuda.current_stream().cuda_stream)
     return out
@@ -349,7 +353,8 @@ def _launch(fn, device, *args):
     """fn(*args, stream) on the current stream of `device`, with that device current."""
     import torch
     index = device.index
-    assert device.type == "cuda"
+    if not (device.type == "cuda"):
+        raise AssertionError("tensors on the GPU")
     if index == torch.cuda.current_device():
         # the stream's address as it is, without the Stream object around it (1.7 us of a call)
         status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
@@ -363,7 +368,8 @@ def _launch(fn, device, *args):
 def _matrix(t, dtype, device) -> int:
     """The row stride of a matrix on `device` whose channels follow each other (a slice of a wider matrix is fine)."""
     stride = t.stride()
-    assert t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or t.shape[1] == 1) and t.device == device
+    if not (t.dtype is dtype and len(stride) == 2 and (stride[1] == 1 or t.shape[1] == 1) and t.device == device):
+        raise AssertionError("matrices of the expected type on one device, whose channels follow each other")
     return stride[0]
 
 
@@ -393,7 +399,8 @@ def _fp8_rows(like, rows: int, channels: int, out):
         return q, q.stride(0), like.new_empty((blocks, rows), dtype=torch.float32), rows
     q, scale = out
     qs, ss = _matrix(q, torch.float8_e4m3fn, like.device), _matrix(scale, torch.float32, like.device)
-    assert q.shape == (rows, channels) and scale.shape == (blocks, rows)
+    if not (q.shape == (rows, channels) and scale.shape == (blocks, rows)):
+        raise AssertionError("out: [rows, channels] and [blocks, rows]")
     return q, _apart(qs, channels, rows), scale, _apart(ss, rows, blocks)
 
 
@@ -411,7 +418,8 @@ def quantize_fp8(x, gated: bool = False, out=None):
     xs = _matrix(x, x.dtype, device)
     rows, channels = x.shape
     if gated:
-        assert channels % 2 == 0
+        if not (channels % 2 == 0):
+            raise AssertionError("rows of gate and up")
         channels //= 2
     if rows | channels > _LARGEST_SIZE:
         _check_sizes(rows, channels)
@@ -431,15 +439,18 @@ def rms_norm_fp8(x, weight, eps: float = 1e-6, residual=None, sum_out=None, out=
     rows, channels = shape = x.shape
     if rows | channels > _LARGEST_SIZE:
         _check_sizes(rows, channels)
-    assert weight.dtype is torch.float32 and weight.shape == (channels,) and weight.is_contiguous() and weight.device == device
+    if not (weight.dtype is torch.float32 and weight.shape == (channels,) and weight.is_contiguous() and weight.device == device):
+        raise AssertionError("weight: fp32 [channels], contiguous, on the device of x")
     xp, rp, rs, hp, hs = x.data_ptr(), 0, 0, 0, 0
     if residual is not None:
         rs = _matrix(residual, xt, device)
-        assert residual.shape == shape
+        if not (residual.shape == shape):
+            raise AssertionError("residual: the shape of x")
         rp = residual.data_ptr()
     if sum_out is not None:
         hs = _apart(_matrix(sum_out, xt, device), channels, rows)
-        assert sum_out.shape == shape
+        if not (sum_out.shape == shape):
+            raise AssertionError("sum_out: the shape of x")
         hp = sum_out.data_ptr()
         if rows == 1:                       # a single row's stride says nothing
             xs = rs = hs
@@ -468,7 +479,8 @@ def quantize_weights_fp8(w, out=None):
     else:
         q, scale = out
         qs = _apart(_matrix(q, torch.float8_e4m3fn, device), k, n)
-        assert q.shape == (n, k) and scale.shape == blocks and scale.dtype is torch.float32 and scale.device == device and scale.is_contiguous()
+        if not (q.shape == (n, k) and scale.shape == blocks and scale.dtype is torch.float32 and scale.device == device and scale.is_contiguous()):
+            raise AssertionError("out: e4m3 [n, k] and fp32 [blocks of n, blocks of k], contiguous, on the device of w")
     _launch(load_library().demon_vae_quantize_weights_fp8, device, w.data_ptr(), ws, n, k, dtype, q.data_ptr(), qs, scale.data_ptr())
     return q, scale
 
@@ -490,14 +502,18 @@ def matmul_fp8(a, a_scale, w, w_scale, bias=None, dtype=None, n_frames: int = 0,
     blocks = -(-k // 128)
     as_, ws = _matrix(a, torch.float8_e4m3fn, device), _matrix(w, torch.float8_e4m3fn, device)
     ss, _ = _matrix(a_scale, torch.float32, device), _matrix(w_scale, torch.float32, device)
-    assert w.shape[1] == k and a_scale.shape == (blocks, rows) and w_scale.shape == (-(-n // 128), blocks) and w_scale.is_contiguous()
-    assert bias is None or (bias.device == device and bias.dtype is torch.float32 and bias.is_contiguous() and bias.shape == (n,))
-    assert n_frames >= 0 and (n_frames == 0 or rows % n_frames == 0)
+    if not (w.shape[1] == k and a_scale.shape == (blocks, rows) and w_scale.shape == (-(-n // 128), blocks) and w_scale.is_contiguous()):
+        raise AssertionError("w: [n, k]; a_scale: [blocks of k, rows]; w_scale: [blocks of n, blocks of k], contiguous")
+    if not (bias is None or (bias.device == device and bias.dtype is torch.float32 and bias.is_contiguous() and bias.shape == (n,))):
+        raise AssertionError("bias: fp32 [n], contiguous, on the device of a")
+    if not (n_frames >= 0 and (n_frames == 0 or rows % n_frames == 0)):
+        raise AssertionError("rows: a multiple of n_frames")
     shape = (rows // n_frames, n, n_frames) if n_frames else (rows, n)
     if out is None:
         out, os_ = a.new_empty(shape, dtype=dtype or torch.bfloat16), n
     else:
-        assert out.shape == shape and out.device == device and (dtype is None or dtype is out.dtype) and (n_frames == 0 or out.is_contiguous())
+        if not (out.shape == shape and out.device == device and (dtype is None or dtype is out.dtype) and (n_frames == 0 or out.is_contiguous())):
+            raise AssertionError("out: the result's shape (a latent contiguous), its type as dtype, on the device of a")
         os_ = 0 if n_frames else _apart(_matrix(out, out.dtype, device), n, rows)
     lib = load_library()
     _launch(lib.demon_vae_matmul_fp8_fp32_sums if fp32_sums else lib.demon_vae_matmul_fp8, device, a.data_ptr(), as_, a_scale.data_ptr(), _apart(ss, rows, blocks), w.data_ptr(), ws,
@@ -570,13 +586,17 @@ class DemonVAE:
         import torch
         if latent.dim() == 2:
             latent = latent[None]
-        assert latent.is_cuda and latent.dtype == self.torch_dtype and latent.is_contiguous()
+        if not (latent.is_cuda and latent.dtype == self.torch_dtype and latent.is_contiguous()):
+            raise AssertionError("latent: contiguous, of the decoder's type, on the GPU")
         n_clips, c, t = latent.shape
-        assert c == self.spec.latent_channels
+        if not (c == self.spec.latent_channels):
+            raise AssertionError("latent: the decoder's channels")
         if out is None:
             out = torch.empty((n_clips, self.spec.out_channels, t * self.S), dtype=torch.float32, device=latent.device)
-        assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()
-        assert tuple(out.shape) == (n_clips, self.spec.out_channels, t * self.S)
+        if not (out.is_cuda and out.dtype == torch.float32 and out.is_contiguous()):
+            raise AssertionError("out: contiguous fp32 on the GPU")
+        if not (tuple(out.shape) == (n_clips, self.spec.out_channels, t * self.S)):
+            raise AssertionError("out: [clips, out channels, samples]")
         return latent, out, n_clips, t, torch.cuda.current_stream().cuda_stream
 
     def decode(self, latent, out=None):
@@ -608,7 +628,8 @@ class DemonVAE:
         """skip: int32 device tensor [n_clips]; clips with a non-zero flag keep what `out` holds."""
         import torch
         latent, out, n_clips, t, stream = self._prep(latent, out)
-        assert skip.is_cuda and skip.dtype == torch.int32 and skip.is_contiguous() and skip.numel() == n_clips
+        if not (skip.is_cuda and skip.dtype == torch.int32 and skip.is_contiguous() and skip.numel() == n_clips):
+            raise AssertionError("skip: one int32 a clip, contiguous, on the GPU")
         if frame_end is None:
             frame_end = t
         demon_vae_decode_windowed_gated(self.handle, latent.data_ptr(), n_clips, t, frame_begin, frame_end, window, halo,
@@ -621,13 +642,17 @@ class DemonVAE:
         import torch
         if latent.dim() == 2:
             latent = latent[None]
-        assert latent.is_cuda and latent.dtype == self.torch_dtype and latent.is_contiguous()
+        if not (latent.is_cuda and latent.dtype == self.torch_dtype and latent.is_contiguous()):
+            raise AssertionError("latent: contiguous, of the decoder's type, on the GPU")
         n_clips, c, t = latent.shape
-        assert c == self.spec.latent_channels
+        if not (c == self.spec.latent_channels):
+            raise AssertionError("latent: the decoder's channels")
         if out is None:
             out = torch.zeros((n_clips, t * self.S, self.spec.out_channels), dtype=torch.int16, device=latent.device)
-        assert out.is_cuda and out.dtype == torch.int16 and out.is_contiguous()
-        assert tuple(out.shape) == (n_clips, t * self.S, self.spec.out_channels)
+        if not (out.is_cuda and out.dtype == torch.int16 and out.is_contiguous()):
+            raise AssertionError("out: contiguous int16 on the GPU")
+        if not (tuple(out.shape) == (n_clips, t * self.S, self.spec.out_channels)):
+            raise AssertionError("out: [clips, samples, out channels]")
         if frame_end is None:
             frame_end = t
         demon_vae_decode_windowed_pcm16(self.handle, latent.data_ptr(), n_clips, t, frame_begin, frame_end, window,
@@ -707,19 +732,24 @@ class DemonVAEEncoder:
         import torch
         if wave.dim() == 2:
             wave = wave[None]
-        assert wave.is_cuda and wave.dtype == torch.float32 and wave.is_contiguous()
+        if not (wave.is_cuda and wave.dtype == torch.float32 and wave.is_contiguous()):
+            raise AssertionError("wave: contiguous fp32 on the GPU")
         n_clips, ch, n = wave.shape
-        assert ch == self.spec.out_channels and n % self.S == 0
+        if not (ch == self.spec.out_channels and n % self.S == 0):
+            raise AssertionError("wave: the encoder's channels, whole frames")
         t = n // self.S
         c0 = self.spec.latent_channels
         if moments is None:
             moments = torch.zeros((n_clips, 2 * c0, t), dtype=torch.float32, device=wave.device)
         if latent is None:
             latent = torch.zeros((n_clips, c0, t), dtype=self.latent_dtype, device=wave.device)
-        assert moments.is_contiguous() and moments.dtype == torch.float32 and tuple(moments.shape) == (n_clips, 2 * c0, t)
-        assert latent.is_contiguous() and latent.dtype == self.latent_dtype and tuple(latent.shape) == (n_clips, c0, t)
+        if not (moments.is_contiguous() and moments.dtype == torch.float32 and tuple(moments.shape) == (n_clips, 2 * c0, t)):
+            raise AssertionError("moments: contiguous fp32 [clips, 2 latent channels, frames]")
+        if not (latent.is_contiguous() and latent.dtype == self.latent_dtype and tuple(latent.shape) == (n_clips, c0, t)):
+            raise AssertionError("latent: contiguous, of the encoder's type, [clips, latent channels, frames]")
         if eps is not None:
-            assert eps.is_cuda and eps.dtype == torch.float32 and eps.is_contiguous() and tuple(eps.shape) == (n_clips, c0, t)
+            if not (eps.is_cuda and eps.dtype == torch.float32 and eps.is_contiguous() and tuple(eps.shape) == (n_clips, c0, t)):
+                raise AssertionError("eps: contiguous fp32 [clips, latent channels, frames] on the GPU")
         if frame_end is None:
             frame_end = t
         demon_vae_encode_windowed(self.handle, wave.data_ptr(), n_clips, t, frame_begin, frame_end, window, halo,
