@@ -408,7 +408,8 @@ DEMON_API demon_status demon_vae_quantize_weights_fp8(const void* d_w, long long
  *   d_out          : device, fp32 or bf16 (out_dtype).  n_frames = 0: [rows][n], rows out_stride elements apart.  n_frames > 0: the
  *                    latent [rows / n_frames][n][n_frames] (the layout demon_vae_decode reads) of rows m = clip * n_frames + frame;
  *                    out_stride is not used
- * INVALID_ARG also if rows is no multiple of n_frames.  UNSUPPORTED: rows, n or k > 16777216.
+ * INVALID_ARG also if rows is no multiple of n_frames.  UNSUPPORTED: rows, n or k > 16777216; more outputs than a launch has threads
+ * for, which are 2^32 (rows rounded up to a multiple of 16, n to one of 32) where rows of d_a or d_w are 4194304 bytes apart or more, and 2^36 or more elsewhere.
  */
 DEMON_API demon_status demon_vae_matmul_fp8(const void* d_a, long long a_stride, const float* d_a_scale, long long a_scale_stride,
                                             const void* d_w, long long w_stride, const float* d_w_scale, const float* d_bias,

@@ -35,7 +35,9 @@ demon_status matmul(const MatmulFp8& a, demon_dtype out_dtype, bool fp32_sums, v
     if (a.n_frames < 0 || (a.n_frames > 0 && a.rows % a.n_frames != 0)) return fail(DEMON_ERR_INVALID_ARG, "rows must be a multiple of n_frames");
     if (a.n_frames == 0 && a.out_stride < a.n) return fail(DEMON_ERR_INVALID_ARG, "output rows overlap");
     if (a.rows > (1 << 24) || a.n > (1 << 24) || a.k > (1 << 24)) return fail(DEMON_ERR_UNSUPPORTED, "more than 16777216 rows, columns or values of K");
-    return launched(launch_matmul_fp8(a, out_dtype == DEMON_BF16, fp32_sums, (hipStream_t)stream), "matrix product");
+    const hipError_t e = launch_matmul_fp8(a, out_dtype == DEMON_BF16, fp32_sums, (hipStream_t)stream);
+    if (e == hipErrorNotSupported) return fail(DEMON_ERR_UNSUPPORTED, "more outputs than a launch has threads for");
+    return launched(e, "matrix product");
 }
 
 }  // namespace

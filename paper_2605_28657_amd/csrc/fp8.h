@@ -18,7 +18,8 @@ hipError_t launch_rms_norm_fp8(const RowsFp8& a, const NormFp8& n, bool bf16, hi
 // weights [n][k] in e4m3 with the scales [blocks of 128 rows][blocks of 128 columns]
 hipError_t launch_quantize_weights_fp8(const void* w, long long w_stride, int n, int k, bool bf16, uint8_t* q, long long q_stride, float* scale,
                                        hipStream_t stream);
-// out = a w^T by the blocks' scales (+ bias), fp32 or bf16; n_frames > 0: out is [rows / n_frames][n][n_frames].  fp32_sums: bf16 outputs' too
+// out = a w^T by the blocks' scales (+ bias), fp32 or bf16; n_frames > 0: out is [rows / n_frames][n][n_frames].  fp32_sums: bf16 outputs' too.
+// hipErrorNotSupported: more outputs than a launch has threads for (nothing was launched)
 struct MatmulFp8 { const uint8_t* a; long long a_stride; const float* a_scale; long long a_scale_stride; const uint8_t* w; long long w_stride;
                    const float* w_scale; const float* bias; void* out; long long out_stride; int rows, n, k, n_frames; };
 hipError_t launch_matmul_fp8(const MatmulFp8& a, bool bf16, bool fp32_sums, hipStream_t stream);

@@ -112,7 +112,7 @@ __device__ __forceinline__ void store_out(uint16_t* p, float v) { *p = f32_to_bf
 __device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_out(Bf16Fp32Sums* p, float v) { p->bits = f32_to_bf16_bits(v); }
 
-// A launch has at most 2^32 - 1 threads.
+// A launch has at most 2^32 - 1 threads.  A product that would take more is hipErrorNotSupported.
 inline bool fits(long long workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
 
 // Where out[m][n] is: rows of n values, or the latent [clip][n][frame] of rows m = clip * n_frames + frame.
@@ -635,7 +635,7 @@ template <bool BIAS> __global__ __launch_bounds__(512, 2) void matmul_rounds_ker
 template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU, int KS = 1> static hipError_t launch_tile(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 16 * FN * WN - 1) / (16 * FN * WN)) * ((a.rows + 16 * FM * WM - 1) / (16 * FM * WM));
-    if (!fits(tiles, 64 * WN * WM * KS)) return hipErrorInvalidValue;
+    if (!fits(tiles, 64 * WN * WM * KS)) return hipErrorNotSupported;
     hipLaunchKernelGGL((matmul_tile_kernel<O, WN, WM, FN, FM, DIRECT, EU, KS>), dim3((unsigned)tiles), dim3(64 * WN * WM * KS), 0, stream, a);
     return hipGetLastError();
 }
@@ -643,7 +643,7 @@ template <typename O, int WN, int WM, int FN, int FM, bool DIRECT, int EU, int K
 static hipError_t launch_rounds(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 255) / 256) * ((a.rows + 255) / 256);
-    if (tiles > 0x7fffffffll) return hipErrorInvalidValue;
+    if (tiles > 0x7fffffffll) return hipErrorNotSupported;
     hipLaunchKernelGGL(a.bias ? matmul_rounds_kernel<true> : matmul_rounds_kernel<false>, dim3(256), dim3(512), 0, stream, a);
     return hipGetLastError();
 }
@@ -651,7 +651,7 @@ static hipError_t launch_rounds(const MatmulFp8& a, hipStream_t stream)
 template <typename O, int FN, int FM, int W, int U> static hipError_t launch_direct(const MatmulFp8& a, hipStream_t stream)
 {
     const long long tiles = (long long)((a.n + 16 * FN - 1) / (16 * FN)) * ((a.rows + 16 * FM - 1) / (16 * FM));
-    if (!fits(tiles, 64 * W)) return hipErrorInvalidValue;
+    if (!fits(tiles, 64 * W)) return hipErrorNotSupported;
     hipLaunchKernelGGL((matmul_direct_kernel<O, FN, FM, W, U>), dim3((unsigned)tiles), dim3(64 * W), 0, stream, a);
     return hipGetLastError();
 }
