@@ -339,8 +339,8 @@ DEMON_API demon_status demon_vae_crossfade(const float* d_prev_tail, long long p
 
 /*
  * ---- Operators of the generator's layers in 8 bits.  In every tick of the streaming loop (section 3.1) the transformer that makes the
- * latents runs before the decode; section 3.7 keeps its norms in fp32 and its products in fewer bits.  These are its norm, its
- * products and the two steps that make their operands, for inference:
+ * latents runs before the decode (in 16 bits with norms in fp32, section 3.7).  These are a transformer layer's norm, its products with operands in 8 bits,
+ * which the paper does not go down to, and the two steps that make these operands, for inference.  The norm has one weight for all rows: no scale or shift of a clip's own.
  *
  *   demon_vae_rms_norm_fp8 -> demon_vae_matmul_fp8 -> demon_vae_quantize_fp8 (gated) -> demon_vae_matmul_fp8 -> (residual of the next norm)
  *
@@ -373,7 +373,8 @@ DEMON_API demon_status demon_vae_quantize_fp8(const void* d_x, long long x_strid
 /*
  * Root-mean-square norm with the residual's addition, its output in 8 bits:
  *   h = x + residual,   y[c] = h[c] / sqrt(mean over the channels of h^2 + eps) * weight[c]
- * in fp32; h is normed as it is, and rounded only for d_sum.  (A row of zeros with eps = 0 is NaN.)
+ * in fp32; h is normed as it is, and rounded only for d_sum.  (A row of zeros with eps = 0 is NaN.  The squares' sum is an fp32 value too: where it overflows
+ * y is zeros, where it vanishes and eps = 0 NaN.)
  *   d_x, d_residual : device, [rows][channels], fp32 or bf16; d_residual NULL: h = x
  *   d_weight        : device, fp32 [channels]
  *   d_sum           : device, h in the type of d_x, or NULL.  May be d_x or d_residual itself (same pointer and stride)
@@ -395,7 +396,8 @@ DEMON_API demon_status demon_vae_quantize_weights_fp8(const void* d_w, long long
 /*
  * Matrix product of 8-bit rows and weights:
  *   out[m][j] = bias[j] + sum over blocks b of a_scale[b][m] w_scale[j / 128][b] * (sum over i in b of a[m][i] w[j][i])
- * the outer sum in fp32, the result rounded to out_dtype to nearest even, in an order that depends on the sizes, alignment and strides alone.  The inner sums:
+ * The product of the two scales and the outer sum are taken in fp32, in an order that depends on the sizes, alignment and strides alone, and the result is rounded to
+ * out_dtype to nearest even.  (Where the scales' product leaves fp32's normal range, 2^-126 to 2^128, so do the result's precision and range.)  The inner sums:
  *   out_dtype DEMON_F32 : in fp32 (products of e4m3 values are exact).
  *   out_dtype DEMON_BF16: by the GPU's 8-bit matrix instructions, at twice the rate.  They add 8 values of i that follow each other, from a multiple of 8 on, with
  *                         13 bits behind the largest of the 8 products, the rest cut off toward zero, and these sums in fp32.  An inner sum is off by

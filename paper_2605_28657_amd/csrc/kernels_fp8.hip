@@ -56,8 +56,9 @@ template <> struct Chunk<float> {
     __device__ void set(int e, float x) { v[e / 4][e % 4] = __float_as_uint(x); }
 };
 
-// Elements 0 .. n - 1 (0 < n < 8) of a chunk, zeros behind them, which no maximum or sum of squares sees.  All are loaded at once, the last one for those that
-// are not there: behind a branch of its own each would wait for the one before (weights of 517 x 1111 in bf16: 8.6 us, so 6.2; norm of 75 x 5631 6.2 -> 5.2).
+// Elements 0 .. n - 1 (0 < n < 8) of a chunk, zeros behind them, which no maximum or sum of squares sees.  The elements of one end are requested together, the last one for those that
+// are not there: behind a branch of its own each would wait for the one before (weights of 517 x 1111 in bf16: 8.6 us, so 6.2; norm of 75 x 5631 6.2 -> 5.2).  Several ends of a
+// thread (rows of the weights, chunks and operands of the norm) are still waited for one after another.
 template <typename T> __device__ __forceinline__ void load_tail(Chunk<T>& c, const T* p, int n)
 {
     T v[7];

@@ -9,9 +9,9 @@
 //     the sums of 8 are added in fp32.  So up to 7 products of 8 lose less than 2^-13 of the largest each: less than 2^-10.2 (7 * 2^-13) of the sum over the groups of 8
 //     of their largest product, and of the sum of all products' magnitudes.  Where products do not cancel that is at most a quarter of the output's rounding of 2^-8, for normal
 //     values 1.3e-5 of the result in the 2-norm; where they do it can be all of the result.  Every 8-bit MFMA of this GPU does the same.  It is what the operands' format is for: twice the
-//     operations a second of 16 bits (12000 x 11264 x 2048 260 to 270 us, with fp32 sums 497);
+//     operations a second of 16 bits (12000 x 11264 x 2048 254 to 270 us, with fp32 sums 480 to 640 by the power limit);
 //   output fp32, or bf16 with fp32 sums (Bf16Fp32Sums): the operands widened to halves, which hold every e4m3 value, and four 16 x 16 x 32 MFMAs of halves, whose
-//     sums keep 2^-23 of the largest product (7e-8 in the 2-norm).  The matrix unit does half as many of these a second.
+//     sums keep 2^-23 of the largest product (6e-8 in the 2-norm).  The matrix unit does half as many of these a second.
 // The weights are the rows of the MFMA's result (operand A) and the rows of `a` its columns (operand B): a lane then holds results of
 // one row of `a`, and the product of the scales is one value a lane and tile.
 //
@@ -84,7 +84,7 @@ __device__ __forceinline__ u32x4 shifted(u32x4 v, int missing)
 }
 
 // A piece of 16 values at p, of which the first `left` belong to a row of k values; zeros for the others, which are not read.  The piece that a row of 16 values or
-// more ends in is the row's last 16 bytes, shifted: one load.  (Byte by byte, each behind a branch of its own, it takes 15 one after another: 600 x 2048 x 2047 by 128 x 64 tiles
+// more ends in is the row's last 16 bytes, shifted: one load a piece.  (Byte by byte, each behind a branch of its own, it takes 15 one after another: 600 x 2048 x 2047 by 128 x 64 tiles
 // 27.5 us, this 20.7.)
 __device__ __forceinline__ u32x4 load_piece(const uint8_t* p, int left, int k)
 {
@@ -155,6 +155,7 @@ template <typename O> __device__ __forceinline__ void store_row(const MatmulFp8&
 // A workgroup of W waves takes 16 FN weight rows by 16 FM rows; each wave sums every W-th block of K, from operands that it loads into
 // registers itself, and the waves' sums are added in their order through LDS.  Reads any alignment and any K.  It is bound by the bytes of the weights where they are many (1 x 32000 x 2048
 // 12.5 us, 5240 GB/s) and by the latency of a launch and of two or three dependent loads where not (1 x 2048 x 2048 3.8 us, an empty launch 2.1).
+// The block that K ends in adds 2 FN + 2 FM, a wave's pieces one after another, each behind its branch (1500 x 64 x 1111 in fp32 7.8 us).
 template <typename O, int FN, int FM, int W, int U>
 __global__ __launch_bounds__(64 * W) void matmul_direct_kernel(MatmulFp8 a)
 {
